@@ -430,6 +430,119 @@ rs_status poa_estimate_noalloc(const rs_config* cfg, const rs_records* records, 
                                int64_t max_windows, double* poa_total_dev,
                                int64_t* n_windows_dev, void* cuda_stream);
 
+/* ------------------------------------------------------------------------
+ * A worker's paged KV cache: what follows a routing decision.  The router
+ * counts the leading 16-token blocks of a prompt that a worker holds (m_ij,
+ * §2.2); the worker then needs block tables and slot maps for the step's
+ * tokens (kv_tables), their K and V in the blocks (kv_append), and attention
+ * over the blocks that reads a prefix which requests share once for all of
+ * them (kv_attend).  The paper assumes a serving engine here and gives no
+ * kernels; layouts and rules below are this library's.
+ *
+ * A step: n_req requests, request i with q_len[i] >= 0 new tokens after
+ * prev_len[i] cached ones, kv_len[i] = prev_len[i] + q_len[i].  The tokens of
+ * request i are rows q_start[i] .. q_start[i+1] - 1 of every per-token array;
+ * rows from q_start[n_req] up to n_tokens belong to no request (a step of
+ * fixed size).  Token t of request i stands at position kv_len[i] - q_len[i]
+ * + t.  All calls are asynchronous on the context stream, read lengths and
+ * tables on the device only, and neither read nor write outside the arrays
+ * described here, whatever the lengths and tables hold.  The workspace of
+ * kv_attend grows at a call larger than those before it (cudaMalloc), so a
+ * stream capture follows one such call outside it. */
+
+enum { RS_BF16 = 0, RS_FP16 = 1 };
+
+/* K and V of one layer.  Element d of kv head h of token s (0..15) of block b
+ * is at b * stride_block + h * stride_head + s * stride_token + d of k and v
+ * (elements; any order of the three, e.g. blocks of [head][token][d] or
+ * [token][head][d], K and V beside each other or apart). */
+typedef struct {
+  void* k;                 /* device, 16-byte aligned; v likewise */
+  void* v;
+  int32_t dtype;           /* RS_BF16 or RS_FP16 */
+  int32_t n_kv_heads;      /* 1 .. 1024 */
+  int32_t head_dim;        /* 64 or 128 */
+  int32_t reserved0;
+  int64_t n_blocks;        /* 1 .. 2^27 */
+  int64_t stride_block, stride_head, stride_token;   /* > 0, multiples of 8, < 2^35 */
+} rs_kv_cache;
+
+/* The requests of one step (device arrays; int32). */
+typedef struct {
+  int32_t n_req;           /* 0 .. 16384 */
+  int32_t n_tokens;        /* rows of the per-token arrays, 0 .. 2^24 */
+  int32_t n_groups;        /* groups of requests with a shared prefix, 0 .. n_req */
+  int32_t max_blocks;      /* entries of a table row, 1 .. 2^24 */
+  int64_t table_stride;    /* entries from row to row, >= max_blocks */
+  int32_t* table;          /* [n_req] rows: block of tokens 16 k .. 16 k + 15 at entry k */
+  int32_t* q_start;        /* [n_req + 1] non-decreasing, first 0 */
+  int32_t* kv_len;         /* [n_req] */
+  /* Group g is requests group_start[g] .. group_start[g+1] - 1 and shares the
+   * blocks of the first floor(prefix_len[g] / 16) table entries; requests
+   * before the first or past the last group have no shared prefix.  Both NULL
+   * when n_groups is 0. */
+  const int32_t* group_start;   /* [n_groups + 1] non-decreasing, within 0 .. n_req */
+  const int32_t* prefix_len;    /* [n_groups] tokens */
+} rs_kv_batch;
+
+/* Block tables, positions and slot maps of a step from the lengths.
+ *   q_len_dev, prev_len_dev: int32 [n_req] (values below 0 count as 0; a
+ *     length past 2^31 - 1 - 16 ends there).
+ *   prefix_blocks_dev: int32 [n_groups][prefix_stride], the block ids of each
+ *     group's shared prefix (NULL without groups; prefix_len[g] / 16 <=
+ *     prefix_stride, longer ones are cut).
+ *   free_dev: int32 [n_free] unused block ids, handed out from the front in
+ *     the order of requests and positions (not written).
+ * Reads the entries of batch->table that hold cached tokens; writes
+ *   table: for every member of a group its prefix's entries; for every request
+ *     entries max(ceil(prev_len / 16), prefix blocks) .. ceil(kv_len / 16) - 1
+ *     from the free list, -1 once that has run out; no other entries;
+ *   q_start, kv_len;
+ *   positions_dev: int32 [n_tokens], -1 on rows of no request;
+ *   slots_dev: int64 [n_tokens], 16 * block + position % 16; -1 on rows of no
+ *     request, without a block, or past the table's row;
+ *   counts_dev: int64 [2]: blocks the step needs (with more than n_free the
+ *     rest is missing above), and its tokens (rows past n_tokens are left out).
+ * Outputs must not overlap inputs. */
+rs_status kv_tables(rs_ctx* ctx, const rs_kv_batch* batch, const int32_t* q_len_dev,
+                    const int32_t* prev_len_dev, const int32_t* prefix_blocks_dev,
+                    int64_t prefix_stride, const int32_t* free_dev, int64_t n_free,
+                    int32_t* positions_dev, int64_t* slots_dev, int64_t* counts_dev);
+
+/* Puts K and V of n_tokens rows into the cache: row r, head h, element d at
+ * r * token_stride + h * head_stride + d of k_dev and v_dev (cache's dtype;
+ * any strides, e.g. columns of one projection) goes to token slots_dev[r] % 16
+ * of block slots_dev[r] / 16.  Rows with a slot outside the cache (-1) are
+ * skipped; two rows with one slot leave either's values. */
+rs_status kv_append(rs_ctx* ctx, const rs_kv_cache* cache, const void* k_dev, const void* v_dev,
+                    int64_t token_stride, int64_t head_stride, int32_t n_tokens,
+                    const int64_t* slots_dev);
+
+/* Causal attention of the step's tokens over the cache's blocks.  Row r = token
+ * t of request i, query head h, kv head h / (n_heads / n_kv_heads):
+ *   out[r][h] = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale q[r][h] . k_j),
+ *   lse[r][h] = log sum_j p_j,
+ * over positions j <= kv_len[i] - q_len + t with q_len = q_start[i+1] -
+ * q_start[i] (the new tokens' K and V are in the cache: kv_append first).  A
+ * row without any position, or of no request, gets 0 and -inf.  Scores,
+ * softmax statistics and sums are in 32 bits; the weights p_j are rounded to
+ * the cache's type for the product with V, and out once at the end.
+ *   q_dev: [n_tokens][n_heads][head_dim] of the cache's type, strides in
+ *     elements, multiples of 8, 16-byte aligned; out_dev likewise.
+ *   lse_dev: float [n_tokens][n_heads], or NULL.
+ *   scale > 0, finite.  n_heads: a multiple of n_kv_heads, at most 128 times it.
+ * The shared prefix of a group is read from the table row of its first
+ * request; the other rows' entries there must be the same.  Where it saves
+ * work, a group's prefix is one product for all the group's rows, joined with
+ * each request's own part by their log sums.  A table entry outside the
+ * cache reads as a block of zeros.  What lies in the blocks past kv_len does
+ * not matter, NaN included; K and V of the kv_len tokens have to be finite
+ * (0 times an infinity in a masked position of the same request is NaN). */
+rs_status kv_attend(rs_ctx* ctx, const rs_kv_cache* cache, const rs_kv_batch* batch,
+                    const void* q_dev, int32_t n_heads, int64_t q_token_stride,
+                    int64_t q_head_stride, float scale, void* out_dev, int64_t out_token_stride,
+                    int64_t out_head_stride, float* lse_dev);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1322,6 +1322,127 @@ rs_status sweep_knee(rs_ctx* ctx, const rs_records* records, const int64_t* row_
   return RS_OK;
 }
 
+// ---------------------------------------------------------------- a worker's KV cache
+
+// The checks of a cache descriptor; a stride along an axis of one entry is
+// never used and becomes the head dimension.
+static rs_status check_cache(rs_ctx* ctx, const rs_kv_cache* c, rs_kv_cache* out) {
+  if (!c) return fail(ctx, RS_ERR_INVALID, "cache is NULL");
+  if (!c->k || !c->v) return fail(ctx, RS_ERR_INVALID, "cache k or v is NULL");
+  if (!aligned16(c->k) || !aligned16(c->v))
+    return fail(ctx, RS_ERR_INVALID, "cache k and v must be 16-byte aligned");
+  if (c->dtype != RS_BF16 && c->dtype != RS_FP16)
+    return fail(ctx, RS_ERR_INVALID, "cache dtype must be RS_BF16 or RS_FP16");
+  if (c->head_dim != 64 && c->head_dim != 128)
+    return fail(ctx, RS_ERR_INVALID, "head_dim must be 64 or 128");
+  if (c->n_kv_heads < 1 || c->n_kv_heads > 1024)
+    return fail(ctx, RS_ERR_INVALID, "n_kv_heads must be in [1, 1024]");
+  if (c->n_blocks < 1 || c->n_blocks > (1ll << 27))
+    return fail(ctx, RS_ERR_INVALID, "n_blocks must be in [1, 2^27]");
+  *out = *c;
+  if (c->n_kv_heads == 1) out->stride_head = c->head_dim;
+  if (c->n_blocks == 1) out->stride_block = c->head_dim;
+  for (int64_t s : {out->stride_block, out->stride_head, out->stride_token})
+    if (s <= 0 || s % 8 != 0 || s >= (1ll << 35))
+      return fail(ctx, RS_ERR_INVALID, "cache strides must be multiples of 8 in (0, 2^35)");
+  return RS_OK;
+}
+
+static rs_status check_batch(rs_ctx* ctx, const rs_kv_batch* b) {
+  if (!b) return fail(ctx, RS_ERR_INVALID, "batch is NULL");
+  if (b->n_req < 0 || b->n_req > 16384)
+    return fail(ctx, RS_ERR_INVALID, "n_req must be in [0, 16384]");
+  if (b->n_tokens < 0 || b->n_tokens > (1 << 24))
+    return fail(ctx, RS_ERR_INVALID, "n_tokens must be in [0, 2^24]");
+  if (b->n_groups < 0 || b->n_groups > b->n_req)
+    return fail(ctx, RS_ERR_INVALID, "n_groups must be in [0, n_req]");
+  if (b->max_blocks < 1 || b->max_blocks > (1 << 24))
+    return fail(ctx, RS_ERR_INVALID, "max_blocks must be in [1, 2^24]");
+  if (b->table_stride < b->max_blocks)
+    return fail(ctx, RS_ERR_INVALID, "table_stride < max_blocks");
+  if (!b->q_start || (b->n_req > 0 && (!b->table || !b->kv_len)))
+    return fail(ctx, RS_ERR_INVALID, "NULL pointer in the batch");
+  if (b->n_groups > 0 && (!b->group_start || !b->prefix_len))
+    return fail(ctx, RS_ERR_INVALID, "groups need group_start and prefix_len");
+  return RS_OK;
+}
+
+rs_status kv_tables(rs_ctx* ctx, const rs_kv_batch* batch, const int32_t* q_len_dev,
+                    const int32_t* prev_len_dev, const int32_t* prefix_blocks_dev,
+                    int64_t prefix_stride, const int32_t* free_dev, int64_t n_free,
+                    int32_t* positions_dev, int64_t* slots_dev, int64_t* counts_dev) {
+  if (!ctx) return fail(nullptr, RS_ERR_INVALID, "ctx is NULL");
+  ctx->err.clear();
+  rs_status r = check_batch(ctx, batch);
+  if (r != RS_OK) return r;
+  if (n_free < 0 || n_free > INT32_MAX) return fail(ctx, RS_ERR_INVALID, "n_free must be in [0, 2^31)");
+  if (prefix_stride < 0) return fail(ctx, RS_ERR_INVALID, "prefix_stride < 0");
+  if (batch->n_groups > 0 && prefix_stride > 0 && !prefix_blocks_dev)
+    return fail(ctx, RS_ERR_INVALID, "groups need prefix_blocks");
+  if ((batch->n_req > 0 && (!q_len_dev || !prev_len_dev)) || (n_free > 0 && !free_dev) || !counts_dev ||
+      (batch->n_tokens > 0 && (!positions_dev || !slots_dev)))
+    return fail(ctx, RS_ERR_INVALID, "NULL pointer");
+  CK(launch_kv_tables(*batch, q_len_dev, prev_len_dev, prefix_blocks_dev, prefix_stride, free_dev, n_free,
+                      positions_dev, slots_dev, counts_dev, ctx->sms, ctx->st),
+     "block tables launch");
+  return RS_OK;
+}
+
+rs_status kv_append(rs_ctx* ctx, const rs_kv_cache* cache, const void* k_dev, const void* v_dev,
+                    int64_t token_stride, int64_t head_stride, int32_t n_tokens,
+                    const int64_t* slots_dev) {
+  if (!ctx) return fail(nullptr, RS_ERR_INVALID, "ctx is NULL");
+  ctx->err.clear();
+  rs_kv_cache c;
+  rs_status r = check_cache(ctx, cache, &c);
+  if (r != RS_OK) return r;
+  if (n_tokens < 0 || n_tokens > (1 << 24))
+    return fail(ctx, RS_ERR_INVALID, "n_tokens must be in [0, 2^24]");
+  if (n_tokens == 0) return RS_OK;
+  if (!k_dev || !v_dev || !slots_dev) return fail(ctx, RS_ERR_INVALID, "NULL pointer");
+  if ((reinterpret_cast<uintptr_t>(k_dev) | reinterpret_cast<uintptr_t>(v_dev)) & 1)
+    return fail(ctx, RS_ERR_INVALID, "k and v must be 2-byte aligned");
+  if (n_tokens == 1) token_stride = 0;
+  if (c.n_kv_heads == 1) head_stride = 0;
+  if (token_stride < 0 || head_stride < 0) return fail(ctx, RS_ERR_INVALID, "negative stride");
+  CK(launch_kv_append(c, k_dev, v_dev, token_stride, head_stride, n_tokens, slots_dev, ctx->st),
+     "KV append launch");
+  return RS_OK;
+}
+
+rs_status kv_attend(rs_ctx* ctx, const rs_kv_cache* cache, const rs_kv_batch* batch,
+                    const void* q_dev, int32_t n_heads, int64_t q_token_stride,
+                    int64_t q_head_stride, float scale, void* out_dev, int64_t out_token_stride,
+                    int64_t out_head_stride, float* lse_dev) {
+  if (!ctx) return fail(nullptr, RS_ERR_INVALID, "ctx is NULL");
+  ctx->err.clear();
+  KvAttendArgs a;
+  rs_status r = check_cache(ctx, cache, &a.c);
+  if (r == RS_OK) r = check_batch(ctx, batch);
+  if (r != RS_OK) return r;
+  a.b = *batch;
+  if (n_heads < 1 || n_heads % a.c.n_kv_heads != 0 || n_heads / a.c.n_kv_heads > 128)
+    return fail(ctx, RS_ERR_INVALID, "n_heads must be 1 to 128 times n_kv_heads");
+  if (!(scale > 0.0f) || !std::isfinite(scale))
+    return fail(ctx, RS_ERR_INVALID, "scale must be finite and > 0");
+  if (a.b.n_tokens == 0) return RS_OK;
+  if (!q_dev || !out_dev) return fail(ctx, RS_ERR_INVALID, "NULL pointer");
+  if (!aligned16(q_dev) || !aligned16(out_dev))
+    return fail(ctx, RS_ERR_INVALID, "q and out must be 16-byte aligned");
+  a.q = q_dev; a.out = out_dev; a.lse = lse_dev;
+  a.n_heads = n_heads; a.scale = scale;
+  const bool one_t = a.b.n_tokens == 1, one_h = n_heads == 1;   // strides never used
+  a.q_ts = one_t ? a.c.head_dim : q_token_stride;
+  a.q_hs = one_h ? a.c.head_dim : q_head_stride;
+  a.o_ts = one_t ? a.c.head_dim : out_token_stride;
+  a.o_hs = one_h ? a.c.head_dim : out_head_stride;
+  for (int64_t s : {a.q_ts, a.q_hs, a.o_ts, a.o_hs})
+    if (s <= 0 || s % 8 != 0 || s >= (1ll << 35))
+      return fail(ctx, RS_ERR_INVALID, "q and out strides must be multiples of 8 in (0, 2^35)");
+  CK(launch_kv_attend(a, ctx->st), "attention launch");
+  return RS_OK;
+}
+
 // The cache of a replica that ran on block ids: its live log entries' hashes,
 // found on the device (the trace's ids and hashes may be gigabytes).
 static rs_status dump_ids(rs_ctx* ctx, int32_t index, int32_t worker, uint64_t* keys_host,

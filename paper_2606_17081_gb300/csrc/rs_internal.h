@@ -275,4 +275,23 @@ cudaError_t launch_route_release(const RouterState& s, const int32_t* worker, co
 cudaError_t launch_clear_tables(uint64_t* keys, uint32_t* stamp, size_t nslots, CacheMeta* meta,
                                 size_t nmeta, cudaStream_t st);
 
+// A worker's paged KV cache (arguments checked by the caller).
+cudaError_t launch_kv_tables(const rs_kv_batch& b, const int32_t* q_len, const int32_t* prev_len,
+                             const int32_t* prefix_blocks, int64_t prefix_stride,
+                             const int32_t* free_ids, int64_t n_free, int32_t* positions,
+                             int64_t* slots, int64_t* counts, int sms, cudaStream_t st);
+cudaError_t launch_kv_append(const rs_kv_cache& c, const void* k, const void* v, int64_t ts, int64_t hs,
+                             int n_tokens, const int64_t* slots, cudaStream_t st);
+struct KvAttendArgs {
+  rs_kv_cache c;
+  rs_kv_batch b;
+  const void* q;
+  void* out;
+  float* lse;               // or NULL
+  int64_t q_ts, q_hs, o_ts, o_hs;
+  int32_t n_heads;
+  float scale;
+};
+cudaError_t launch_kv_attend(const KvAttendArgs& a, cudaStream_t st);
+
 }  // namespace rs

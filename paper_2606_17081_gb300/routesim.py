@@ -25,6 +25,7 @@ RS_MEM_DEVICE, RS_MEM_HOST = 0, 1
 RS_EVICT_LRU, RS_EVICT_FREQ = 0, 1
 RS_SIM_NO_POA = 1
 RS_SIM_TABLES = 2
+RS_BF16, RS_FP16 = 0, 1
 
 
 class rs_config(C.Structure):
@@ -89,10 +90,24 @@ class rs_timing(C.Structure):
                 ("total_ms", C.c_float), ("launches", C.c_int64), ("hashed_tokens", C.c_int64)]
 
 
+class rs_kv_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("dtype", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("reserved0", C.c_int32),
+                ("n_blocks", C.c_int64), ("stride_block", C.c_int64), ("stride_head", C.c_int64),
+                ("stride_token", C.c_int64)]
+
+
+class rs_kv_batch(C.Structure):
+    _fields_ = [("n_req", C.c_int32), ("n_tokens", C.c_int32), ("n_groups", C.c_int32),
+                ("max_blocks", C.c_int32), ("table_stride", C.c_int64), ("table", C.c_void_p),
+                ("q_start", C.c_void_p), ("kv_len", C.c_void_p), ("group_start", C.c_void_p),
+                ("prefix_len", C.c_void_p)]
+
+
 EXPORTS = ["rs_config_default", "route_init", "route_destroy", "route_last_error",
            "route_hash_blocks", "route_dup_flags", "route_batch", "route_probe", "route_release", "route_active",
            "simulate_replicas", "poa_estimate", "route_cache_dump", "route_last_timing",
-           "poa_estimate_noalloc", "sweep_knee"]
+           "poa_estimate_noalloc", "sweep_knee", "kv_tables", "kv_append", "kv_attend"]
 
 _lib = None
 
@@ -134,6 +149,10 @@ def lib():
                                            vp, vp, i64, vp, vp, vp]),
             "sweep_knee": (i32, [vp, C.POINTER(rs_records), vp, i32, vp, vp, i32, i32,
                                  C.c_double, vp, vp, vp, vp, vp]),
+            "kv_tables": (i32, [vp, C.POINTER(rs_kv_batch), vp, vp, vp, i64, vp, i64, vp, vp, vp]),
+            "kv_append": (i32, [vp, C.POINTER(rs_kv_cache), vp, vp, i64, i64, i32, vp]),
+            "kv_attend": (i32, [vp, C.POINTER(rs_kv_cache), C.POINTER(rs_kv_batch), vp, i32, i64,
+                                i64, C.c_float, vp, i64, i64, vp]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)
@@ -290,6 +309,137 @@ def poa_estimate_noalloc(cfg: rs_config, records: rs_records, n: int, numer_dev,
                                     C.c_void_p(stream or None))
     if st != RS_OK:
         raise RoutesimError(st, "poa_estimate_noalloc rejected the call")
+
+
+# ----------------------------------------------------------------- a worker's KV cache
+
+def _refuse(what: str):
+    raise RoutesimError(RS_ERR_INVALID, what)
+
+
+def _is_dev(x, dtype, what: str, dims: int = 1):
+    """The C entry points see pointers only: type, place and shape are checked here."""
+    if not x.is_cuda or x.dtype != dtype or x.dim() != dims or (dims and x.stride(-1) != 1 and x.size(-1) > 1):
+        _refuse(f"{what} must be a {dims}-dimensional {dtype} tensor on the GPU with unit last stride")
+
+
+class KVCache:
+    """Descriptor of one layer's paged cache, given as views [block, kv head,
+    token in block (16), head_dim] of any strides (unit last stride), e.g.
+    `blocks[:, 0]` of [block, 2, kv head, 16, head_dim] storage, or
+    `blocks.transpose(1, 2)` of token-major blocks.  Keeps the tensors alive."""
+
+    def __init__(self, k, v):
+        import torch
+        types = {torch.bfloat16: RS_BF16, torch.float16: RS_FP16}
+        if k.dtype not in types:
+            _refuse("the cache must be bfloat16 or float16")
+        _is_dev(k, k.dtype, "k", 4)
+        _is_dev(v, k.dtype, "v", 4)
+        if k.shape != v.shape or k.stride() != v.stride() or k.shape[2] != 16:
+            _refuse("k and v must have one shape [block, kv head, 16, head_dim] and one set of strides")
+        self.k, self.v = k, v
+        self.desc = rs_kv_cache(k.data_ptr(), v.data_ptr(), types[k.dtype], k.shape[1], k.shape[3], 0,
+                                k.shape[0], k.stride(0), k.stride(1), k.stride(2))
+        self.ref = C.byref(self.desc)
+
+
+class KVBatch:
+    """Descriptor of a step's requests: table [n_req, max_blocks], q_start
+    [n_req + 1], kv_len [n_req], and, of groups that share a prefix,
+    group_start [n_groups + 1] and prefix_len [n_groups] (all int32, on the
+    GPU); n_tokens rows in the per-token arrays.  Keeps the tensors alive."""
+
+    def __init__(self, table, q_start, kv_len, n_tokens: int, group_start=None, prefix_len=None):
+        import torch
+        _is_dev(table, torch.int32, "table", 2)
+        _is_dev(q_start, torch.int32, "q_start")
+        _is_dev(kv_len, torch.int32, "kv_len")
+        n = table.shape[0]
+        groups = 0
+        if group_start is not None or prefix_len is not None:
+            if group_start is None or prefix_len is None:
+                _refuse("group_start and prefix_len go together")
+            _is_dev(group_start, torch.int32, "group_start")
+            _is_dev(prefix_len, torch.int32, "prefix_len")
+            groups = prefix_len.numel()
+            if group_start.numel() != groups + 1:
+                _refuse("group_start has one entry more than prefix_len")
+        if q_start.numel() != n + 1 or kv_len.numel() != n:
+            _refuse("q_start has n_req + 1 entries and kv_len n_req")
+        self.tensors = (table, q_start, kv_len, group_start, prefix_len)
+        self.n_tokens = n_tokens
+        self.desc = rs_kv_batch(n, n_tokens, groups, table.shape[1],
+                                table.stride(0) if n > 1 else table.shape[1], table.data_ptr(),
+                                q_start.data_ptr(), kv_len.data_ptr(),
+                                group_start.data_ptr() if groups else None,
+                                prefix_len.data_ptr() if groups else None)
+        self.ref = C.byref(self.desc)
+
+
+def kv_tables(ctx, batch: KVBatch, q_len, prev_len, prefix_blocks, free, positions, slots,
+              counts) -> None:
+    """Fills batch's table, q_start and kv_len, and positions int32 [n_tokens],
+    slots int64 [n_tokens], counts int64 [2] (blocks needed, tokens).
+    prefix_blocks: int32 [n_groups, longest prefix in blocks] or None; free: int32."""
+    import torch
+    n = batch.desc.n_req
+    for x, what in ((q_len, "q_len"), (prev_len, "prev_len")):
+        _is_dev(x, torch.int32, what)
+        if x.numel() != n:
+            _refuse(f"{what} has n_req entries")
+    _is_dev(free, torch.int32, "free")
+    _is_dev(positions, torch.int32, "positions")
+    _is_dev(slots, torch.int64, "slots")
+    _is_dev(counts, torch.int64, "counts")
+    if positions.numel() != batch.n_tokens or slots.numel() != batch.n_tokens or counts.numel() != 2:
+        _refuse("positions and slots have n_tokens entries, counts 2")
+    pb, ps = None, 0
+    if batch.desc.n_groups:
+        _is_dev(prefix_blocks, torch.int32, "prefix_blocks", 2)
+        if prefix_blocks.shape[0] != batch.desc.n_groups:
+            _refuse("prefix_blocks has a row a group")
+        pb, ps = prefix_blocks.data_ptr(), prefix_blocks.shape[1]
+        if prefix_blocks.shape[0] > 1 and prefix_blocks.stride(0) != ps:
+            _refuse("prefix_blocks must be contiguous")
+    st = lib().kv_tables(ctx, batch.ref, q_len.data_ptr(), prev_len.data_ptr(), pb, ps,
+                         free.data_ptr(), free.numel(), positions.data_ptr(), slots.data_ptr(),
+                         counts.data_ptr())
+    if st != RS_OK:
+        _check(st, ctx)
+
+
+def kv_append(ctx, cache: KVCache, k, v, slots) -> None:
+    """k, v [n_tokens, kv heads, head_dim] into the cache at slots int64 [n_tokens]."""
+    import torch
+    d = cache.desc
+    _is_dev(k, cache.k.dtype, "k", 3)
+    _is_dev(v, cache.k.dtype, "v", 3)
+    _is_dev(slots, torch.int64, "slots")
+    if k.shape != v.shape or k.stride() != v.stride() or tuple(k.shape) != (slots.numel(), d.n_kv_heads, d.head_dim):
+        _refuse("k and v must be [n_tokens, kv heads, head_dim] of one set of strides, slots [n_tokens]")
+    st = lib().kv_append(ctx, cache.ref, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
+                         k.shape[0], slots.data_ptr())
+    if st != RS_OK:
+        _check(st, ctx)
+
+
+def kv_attend(ctx, cache: KVCache, batch: KVBatch, q, scale: float, out, lse=None) -> None:
+    """q, out [n_tokens, heads, head_dim] of the cache's type; lse float32 [n_tokens, heads] or None."""
+    import torch
+    _is_dev(q, cache.k.dtype, "q", 3)
+    _is_dev(out, cache.k.dtype, "out", 3)
+    if q.shape != out.shape or q.shape[0] != batch.n_tokens or q.shape[2] != cache.desc.head_dim:
+        _refuse("q and out must be [n_tokens, heads, head_dim]")
+    if lse is not None:
+        _is_dev(lse, torch.float32, "lse", 2)
+        if lse.shape != q.shape[:2] or not lse.is_contiguous():
+            _refuse("lse must be a contiguous [n_tokens, heads]")
+    st = lib().kv_attend(ctx, cache.ref, batch.ref, q.data_ptr(), q.shape[1], q.stride(0), q.stride(1),
+                         scale, out.data_ptr(), out.stride(0), out.stride(1),
+                         lse.data_ptr() if lse is not None else None)
+    if st != RS_OK:
+        _check(st, ctx)
 
 
 # ----------------------------------------------------------------- marshalling helpers
