@@ -537,7 +537,9 @@ rs_status kv_append(rs_ctx* ctx, const rs_kv_cache* cache, const void* k_dev, co
  * each request's own part by their log sums.  A table entry outside the
  * cache reads as a block of zeros.  What lies in the blocks past kv_len does
  * not matter, NaN included; K and V of the kv_len tokens have to be finite
- * (0 times an infinity in a masked position of the same request is NaN). */
+ * (0 times an infinity in a masked position of the same request is NaN).
+ * RS_ERR_TIMEOUT: a kernel of an earlier call gave up on a bounded wait (its
+ * outputs are unspecified); reported once, without doing this call's work. */
 rs_status kv_attend(rs_ctx* ctx, const rs_kv_cache* cache, const rs_kv_batch* batch,
                     const void* q_dev, int32_t n_heads, int64_t q_token_stride,
                     int64_t q_head_stride, float scale, void* out_dev, int64_t out_token_stride,

@@ -49,6 +49,8 @@ struct rs_ctx {
   DevBuf p_cost, p_order, p_asg, p_wkey, p_wstart, p_wfill, p_wnum, p_wopt, p_wcnt, p_total,
       p_nwin, p_prob, p_wstat, p_tstat, p_wprob, p_wnext;
   DevBuf k_in, k_out;
+  DevBuf kv_ws;                // kv_attend's workspace
+  int32_t* kv_err = nullptr;   // pinned, written by kv_attend's kernel when a wait ran out
   DevBuf h_tokens, h_offsets, h_release, h_outlen;
   int64_t* pinned = nullptr;   // small host staging for device -> host reads
   size_t pinned_n = 0;
@@ -326,9 +328,10 @@ void route_destroy(rs_ctx* ctx) {
                    &ctx->h_release, &ctx->h_outlen, &ctx->k_in, &ctx->k_out,
                    &ctx->fexp, &ctx->tmpe, &ctx->djobs, &ctx->h_hashes, &ctx->i_jobs, &ctx->i_keys,
                    &ctx->i_first, &ctx->i_num, &ctx->i_ids, &ctx->i_nz, &ctx->i_count,
-                   &ctx->i_stamps, &ctx->i_scratch};
+                   &ctx->i_stamps, &ctx->i_scratch, &ctx->kv_ws};
   for (DevBuf* b : all) release(*b);
   if (ctx->pinned) cudaFreeHost(ctx->pinned);
+  if (ctx->kv_err) cudaFreeHost(ctx->kv_err);
   for (auto& ev : ctx->ev)
     if (ev) cudaEventDestroy(ev);
   delete ctx;
@@ -1439,7 +1442,16 @@ rs_status kv_attend(rs_ctx* ctx, const rs_kv_cache* cache, const rs_kv_batch* ba
   for (int64_t s : {a.q_ts, a.q_hs, a.o_ts, a.o_hs})
     if (s <= 0 || s % 8 != 0 || s >= (1ll << 35))
       return fail(ctx, RS_ERR_INVALID, "q and out strides must be multiples of 8 in (0, 2^35)");
-  CK(launch_kv_attend(a, ctx->st), "attention launch");
+  if (!ctx->kv_err) {
+    CK(cudaMallocHost(reinterpret_cast<void**>(&ctx->kv_err), sizeof(int32_t)), "cudaMallocHost");
+    *ctx->kv_err = 0;
+  }
+  if (*static_cast<volatile int32_t*>(ctx->kv_err)) {
+    *ctx->kv_err = 0;
+    return fail(ctx, RS_ERR_TIMEOUT, "an earlier kv_attend gave up waiting for its own copies or products");
+  }
+  if ((r = ensure(ctx, ctx->kv_ws, kv_attend_bytes(a, ctx->sms), "attention workspace")) != RS_OK) return r;
+  CK(launch_kv_attend(a, ctx->kv_ws.p, ctx->kv_err, ctx->sms, ctx->st), "attention launch");
   return RS_OK;
 }
 

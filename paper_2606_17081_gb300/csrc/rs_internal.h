@@ -292,6 +292,9 @@ struct KvAttendArgs {
   int32_t n_heads;
   float scale;
 };
-cudaError_t launch_kv_attend(const KvAttendArgs& a, cudaStream_t st);
+// ws: kv_attend_bytes of device memory; err: host memory, set to 1 when a
+// bounded wait on the device ran out.
+size_t kv_attend_bytes(const KvAttendArgs& a, int sms);
+cudaError_t launch_kv_attend(const KvAttendArgs& a, void* ws, int32_t* err, int sms, cudaStream_t st);
 
 }  // namespace rs

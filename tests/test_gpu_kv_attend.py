@@ -27,6 +27,8 @@ BF, HF = torch.bfloat16, torch.float16
 def ctx():
     c = rs.Context(W=1, K=1024)
     yield c
+    torch.cuda.synchronize()
+    attend(c, Step(0, [1], [3], 1, 1, 64, BF))   # (would report a wait that ran out in a call before)
     c.close()
 
 
