@@ -351,6 +351,12 @@ __device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatil
   mbar_lost(lost, err);
 }
 
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0;
+}
+
 __device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap* m, int x, int y, int z, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
@@ -401,7 +407,11 @@ __device__ __forceinline__ void tm_st32(uint32_t addr, const uint32_t* v) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], " N32 ";"
                ::R8(v, 0), R8(v, 8), R8(v, 16), R8(v, 24), "r"(addr) : "memory");
 }
-__device__ __forceinline__ void tm_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// Until the loads so far have come; v (one of them) is not touched before.
+#define U8(v, o) "+r"(v[o]), "+r"(v[o + 1]), "+r"(v[o + 2]), "+r"(v[o + 3]), "+r"(v[o + 4]), "+r"(v[o + 5]), "+r"(v[o + 6]), "+r"(v[o + 7])
+__device__ __forceinline__ void tm_wait_ld(uint32_t* v) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : U8(v, 0), U8(v, 8), U8(v, 16), U8(v, 24)::"memory");
+}
 __device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ float ex2(float x) {
@@ -423,6 +433,70 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   if (HALF) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
+}
+
+// ------------------------------------------------------------------ a row's tile of scores
+
+// Keys from `left` on are out of the row's sight.
+__device__ __forceinline__ void cut32(uint32_t* v, int left) {
+#pragma unroll
+  for (int k = 0; k < 32; k++)
+    if (k >= left) v[k] = 0xFF800000u;
+}
+__device__ __forceinline__ float max3(float a, uint32_t b, uint32_t c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(__uint_as_float(b)), "f"(__uint_as_float(c)));
+  return r;
+}
+
+// The largest score of a row's tile.
+__device__ __forceinline__ float row_max(uint32_t ts, bool cut, int left) {
+  uint32_t v[2][32];
+  float m = -INFINITY, n = -INFINITY;
+  tm_ld32(v[0], ts);
+#pragma unroll
+  for (int c = 0; c < 4; c++) {
+    uint32_t* x = v[c & 1];
+    tm_wait_ld(x);
+    if (c < 3) tm_ld32(v[(c + 1) & 1], ts + 32 * (c + 1));
+    if (cut) cut32(x, left - 32 * c);
+#pragma unroll
+    for (int k = 0; k < 32; k += 4) {
+      m = max3(m, x[k], x[k + 1]);
+      n = max3(n, x[k + 2], x[k + 3]);
+    }
+  }
+  return fmaxf(m, n);
+}
+
+// The row's weights exp2(sl s + nm), packed into v's first half, and their sums
+// (of even and odd keys).
+template <bool HALF>
+__device__ __forceinline__ void row_exp(uint32_t ts, bool cut, int left, float sl, float nm, uint32_t* v,
+                                        float& a0, float& a1) {
+  float b0 = 0.0f, b1 = 0.0f;
+  a0 = a1 = 0.0f;
+#pragma unroll
+  for (int c = 0; c < 128; c += 32) tm_ld32(v + c, ts + c);
+#pragma unroll
+  for (int c = 0; c < 128; c += 32) tm_wait_ld(v + c);
+  if (cut) {
+#pragma unroll
+    for (int c = 0; c < 128; c += 32) cut32(v + c, left - c);
+  }
+#pragma unroll
+  for (int k = 0; k < 128; k += 4) {
+    float e0 = __uint_as_float(v[k]), e1 = __uint_as_float(v[k + 1]), e2 = __uint_as_float(v[k + 2]),
+          e3 = __uint_as_float(v[k + 3]);
+    fma2(e0, e1, sl, nm);
+    fma2(e2, e3, sl, nm);
+    e0 = ex2(e0); e1 = ex2(e1); e2 = ex2(e2); e3 = ex2(e3);
+    add2(a0, a1, e0, e1);
+    add2(b0, b1, e2, e3);
+    v[k / 2] = pack2<HALF>(e0, e1);
+    v[k / 2 + 1] = pack2<HALF>(e2, e3);
+  }
+  add2(a0, a1, b0, b1);
 }
 
 // ------------------------------------------------------------------ the kernel
@@ -502,8 +576,9 @@ __device__ __forceinline__ int vplace(int t, int n) { return min(2 * t + 2, 2 * 
 // and 4-7 are the streams' softmax, a thread a row; warp 8 issues the products and
 // warp 9 the loads.
 // TMEM: S of each stream 128 columns (P, 64 columns, overwrites it), O D each.
-// The running maximum of a row is moved only when a tile exceeds it by 2^8 and
-// more, which hardly happens after the first tile: O is scaled then.
+// The m of a row is the largest score of its first tile and moves only when a
+// tile's weights sum to more than 2^15 (each is then below it, in range of
+// fp16), which hardly happens: O and l are scaled then.
 template <int D, bool HALF>
 __global__ void __launch_bounds__(NT_ATT, 1)
 k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
@@ -512,7 +587,7 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
   using L = Lay<D>;
   extern __shared__ __align__(1024) unsigned char sm[];
   const uint32_t base = smem_u32(sm);
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;
   const uint32_t bars = base + L::MISC;
   const uint32_t FULL = bars, EMPTY = bars + 8 * L::NST, QFULL = bars + 16 * L::NST, QEMPTY = QFULL + 16,
                  SFULL = QFULL + 32, PFULL = QFULL + 48, OFULL = QFULL + 64, OEMPTY = QFULL + 80;
@@ -620,57 +695,61 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
         loads += 2 * nt;
       }
     } else if (warp == 8) {
-      // ---------------- products
-      if (lane == 0) {
-        constexpr uint32_t FMT = HALF ? 0u : 1u;
-        constexpr uint32_t IQK = (1u << 4) | (FMT << 7) | (FMT << 10) | ((TK / 8) << 17) | ((128 / 16) << 24);
-        constexpr uint32_t IPV = (1u << 4) | (FMT << 7) | (FMT << 10) | (1u << 16) | ((D / 8) << 17) | ((128 / 16) << 24);
-        uint32_t qn = 0, np[2] = {0, 0}, segs = 0;
-        while (w.next() && !*lost) {
-          const bool wide = w.job.ntok > p.tpt;
-          const int nt = w.t1 - w.t0, E = wide ? 2 * nt : nt;
-          auto qk = [&](int e) {
-            const int s = e & 1, t = wide ? e >> 1 : e;
-            const uint32_t x = loads + kplace(t), slot = (qn + (wide ? s : 0)) & 1;
-            if (!wide || s == 0) mbar_wait(FULL + 8 * (x % L::NST), (x / L::NST) & 1, lost, p.err);
-            if (t == 0) mbar_wait(QFULL + 8 * slot, ((qn + (wide ? s : 0)) >> 1) & 1, lost, p.err);
-            tc_after();
-            const uint32_t qa = base + slot * L::QSLOT, ka = base + L::RING + (x % L::NST) * L::STAGE;
+      // ---------------- products (the warp as one; one thread issues)
+      constexpr uint32_t FMT = HALF ? 0u : 1u;
+      constexpr uint32_t IQK = (1u << 4) | (FMT << 7) | (FMT << 10) | ((TK / 8) << 17) | ((128 / 16) << 24);
+      constexpr uint32_t IPV = (1u << 4) | (FMT << 7) | (FMT << 10) | (1u << 16) | ((D / 8) << 17) | ((128 / 16) << 24);
+      const uint64_t dq = smem_desc(base, 16), dk = smem_desc(base + L::RING, 16),
+                     dv = smem_desc(base + L::RING, TK * 128);
+      uint32_t qn = 0, np[2] = {0, 0}, segs = 0;
+      while (w.next() && !*lost) {
+        const bool wide = w.job.ntok > p.tpt;
+        const int nt = w.t1 - w.t0, E = wide ? 2 * nt : nt;
+        auto qk = [&](int e) {
+          const uint32_t s = e & 1, t = wide ? e >> 1 : e;
+          const uint32_t x = loads + kplace(t), slot = (qn + (wide ? s : 0)) & 1, st = x % L::NST;
+          if (!wide || s == 0) mbar_wait(FULL + 8 * st, (x / L::NST) & 1, lost, p.err);
+          if (t == 0) mbar_wait(QFULL + 8 * slot, ((qn + (wide ? s : 0)) >> 1) & 1, lost, p.err);
+          tc_after();
+          const uint64_t qa = dq + slot * (L::QSLOT >> 4), ka = dk + st * (L::STAGE >> 4);
+          if (elect_one()) {
 #pragma unroll
             for (int k = 0; k < D / 16; k++) {
-              const uint32_t o = (k >> 2) * (128 * 128) + (k & 3) * 32;
-              mma_ss(tmem + s * 128, smem_desc(qa + o, 16), smem_desc(ka + o, 16), IQK, k > 0);
+              const uint32_t o = ((k >> 2) * (128 * 128) + (k & 3) * 32) >> 4;
+              mma_ss(tmem + s * 128, qa + o, ka + o, IQK, k > 0);
             }
             mma_commit(SFULL + 8 * s);
-            if (!wide || s == 1) mma_commit(EMPTY + 8 * (x % L::NST));
+            if (!wide || s == 1) mma_commit(EMPTY + 8 * st);
             if (t == nt - 1) mma_commit(QEMPTY + 8 * slot);
-          };
-          qk(0);
-          if (E > 1) qk(1);
-          for (int e = 0; e < E; e++) {
-            const int s = e & 1, t = wide ? e >> 1 : e;
-            const uint32_t x = loads + vplace(t, nt);
-            if (!wide || s == 0) mbar_wait(FULL + 8 * (x % L::NST), (x / L::NST) & 1, lost, p.err);
-            if (e == 0 && segs > 0) mbar_wait(OEMPTY, (segs - 1) & 1, lost, p.err);
-            mbar_wait(PFULL + 8 * s, np[s] & 1, lost, p.err);
-            np[s]++;
-            tc_after();
-            const uint32_t va = base + L::RING + (x % L::NST) * L::STAGE;
-            const bool first = wide ? t == 0 : e < 2;
+          }
+          __syncwarp();
+        };
+        qk(0);
+        if (E > 1) qk(1);
+        for (int e = 0; e < E; e++) {
+          const uint32_t s = e & 1, t = wide ? e >> 1 : e;
+          const uint32_t x = loads + vplace(t, nt), st = x % L::NST;
+          if (!wide || s == 0) mbar_wait(FULL + 8 * st, (x / L::NST) & 1, lost, p.err);
+          if (e == 0 && segs > 0) mbar_wait(OEMPTY, (segs - 1) & 1, lost, p.err);
+          mbar_wait(PFULL + 8 * s, (s ? np[1] : np[0]) & 1, lost, p.err);
+          if (s) np[1]++; else np[0]++;
+          tc_after();
+          const uint64_t va = dv + st * (L::STAGE >> 4);
+          const uint32_t more = wide ? t > 0 : e >= 2;   // O holds something
+          if (elect_one()) {
 #pragma unroll
             for (int k = 0; k < TK / 16; k++)
-              mma_ts(tmem + 256 + s * D, tmem + s * 128 + k * 8, smem_desc(va + k * 2048, TK * 128), IPV,
-                     !(first && k == 0));
-            if (!wide || s == 1) mma_commit(EMPTY + 8 * (x % L::NST));
+              mma_ts(tmem + 256 + s * D, tmem + s * 128 + k * 8, va + k * (2048 >> 4), IPV, k > 0 ? 1u : more);
+            if (!wide || s == 1) mma_commit(EMPTY + 8 * st);
             if (e + 2 >= E) mma_commit(OFULL + 8 * s);
-            if (e + 2 < E) qk(e + 2);
           }
-          qn += wide ? 2 : 1;
-          segs++;
-          loads += 2 * nt;
+          __syncwarp();
+          if (e + 2 < E) qk(e + 2);
         }
+        qn += wide ? 2 : 1;
+        segs++;
+        loads += 2 * nt;
       }
-      __syncwarp();
     }
   } else {
     // ---------------- softmax, a thread a row
@@ -679,7 +758,6 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t ts = tmem + lanes + s * 128;
     const float sl = __fmul_rn(a.scale, 1.4426950408889634f);
-    const float grow = __fdiv_rn(8.0f, sl);
     float2* ml = reinterpret_cast<float2*>(sm + L::ML);
     uint32_t ns = 0, no[2] = {0, 0}, loads = 0;
     Walk w(p, a.c.n_kv_heads);
@@ -711,47 +789,38 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
       // keys of a last tile that the job's end cuts
       const int ends = w.t1 == w.job.nt ? (w.job.kend - w.job.key0) & (TK - 1) : 0;
       const int low = __reduce_min_sync(~0u, live ? lim : INT_MAX);
-      float m = -INFINITY, l0 = 0.0f, l1 = 0.0f;
+      float m = live ? -INFINITY : 0.0f, l0 = 0.0f, l1 = 0.0f;
       for (int t = wide ? 0 : s; t < nt; t += wide ? 1 : 2) {
         mbar_wait(SFULL + 8 * s, ns & 1, lost, p.err);
         ns++;
         tc_after();
         if (any) {
-          uint32_t v[128];
-#pragma unroll
-          for (int c = 0; c < 4; c++) tm_ld32(v + 32 * c, ts + 32 * c);
-          tm_wait_ld();
           const int k0 = (w.t0 + t) * TK;
-          if (low < k0 + TK) {   // (the warp's rows see different ends)
-            const int left = lim - k0;
-#pragma unroll
-            for (int c = 0; c < 128; c++)
-              if (c >= left) v[c] = 0xFF800000u;
+          const bool cut = low < k0 + TK;   // (the warp's rows see different ends)
+          const int left = lim - k0;
+          const bool first = wide ? t == 0 : t < 2;   // O holds nothing yet
+          if (first) {
+            const float x = row_max(ts, cut, left);
+            if (live) m = x;
           }
-          float x0 = __uint_as_float(v[0]), x1 = __uint_as_float(v[1]), x2 = __uint_as_float(v[2]),
-                x3 = __uint_as_float(v[3]);
-#pragma unroll
-          for (int c = 4; c < 128; c += 8) {
-            x0 = fmaxf(fmaxf(x0, __uint_as_float(v[c])), __uint_as_float(v[c + 1]));
-            x1 = fmaxf(fmaxf(x1, __uint_as_float(v[c + 2])), __uint_as_float(v[c + 3]));
-            if (c + 4 < 128) {
-              x2 = fmaxf(fmaxf(x2, __uint_as_float(v[c + 4])), __uint_as_float(v[c + 5]));
-              x3 = fmaxf(fmaxf(x3, __uint_as_float(v[c + 6])), __uint_as_float(v[c + 7]));
-            }
-          }
-          const float mx = fmaxf(fmaxf(x0, x1), fmaxf(x2, x3));
-          // (also from -inf, at the first tile with a key for the row)
-          if (__any_sync(~0u, __fsub_rn(mx, m) > grow)) {
-            const float m2 = fmaxf(m, mx);
-            if (t >= 2 || (wide && t > 0)) {   // O holds something
-              const float f = m == m2 ? 1.0f : ex2(__fmul_rn(__fsub_rn(m, m2), sl));
+          uint32_t pk[128];
+          float a0, a1;
+          for (;;) {
+            row_exp<HALF>(ts, cut, left, sl, m == -INFINITY ? 0.0f : -__fmul_rn(m, sl), pk, a0, a1);
+            const bool over = live && __fadd_rn(a0, a1) > 32768.0f, none = m == -INFINITY && left > 0;
+            if (!__any_sync(~0u, over || none)) break;
+            const float x = row_max(ts, cut, left);
+            const float m2 = over || none ? fmaxf(m, x) : m;
+            if (!__any_sync(~0u, m2 != m)) break;   // (an infinity: no larger m)
+            const float f = m == m2 ? 1.0f : ex2(__fmul_rn(__fsub_rn(m, m2), sl));
+            if (!first) {
               l0 = __fmul_rn(l0, f);
               l1 = __fmul_rn(l1, f);
 #pragma unroll 1
               for (int c = 0; c < D; c += 32) {
                 uint32_t o[32];
                 tm_ld32(o, tmem + lanes + 256 + s * D + c);
-                tm_wait_ld();
+                tm_wait_ld(o);
 #pragma unroll
                 for (int k = 0; k < 32; k++) o[k] = __float_as_uint(__fmul_rn(__uint_as_float(o[k]), f));
                 tm_st32(tmem + lanes + 256 + s * D + c, o);
@@ -759,24 +828,10 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
             }
             m = m2;
           }
-          const float nm = m == -INFINITY ? 0.0f : -__fmul_rn(m, sl);
-          float a0 = 0.0f, a1 = 0.0f, b0 = 0.0f, b1 = 0.0f;
-#pragma unroll
-          for (int c = 0; c < 128; c += 4) {
-            float e0 = __uint_as_float(v[c]), e1 = __uint_as_float(v[c + 1]), e2 = __uint_as_float(v[c + 2]),
-                  e3 = __uint_as_float(v[c + 3]);
-            fma2(e0, e1, sl, nm);
-            fma2(e2, e3, sl, nm);
-            e0 = ex2(e0); e1 = ex2(e1); e2 = ex2(e2); e3 = ex2(e3);
-            add2(a0, a1, e0, e1);
-            add2(b0, b1, e2, e3);
-            v[c / 2] = pack2<HALF>(e0, e1);
-            v[c / 2 + 1] = pack2<HALF>(e2, e3);
-            if (c == 60) tm_st32(ts, v);
-          }
-          tm_st32(ts + 32, v + 32);
-          l0 = __fadd_rn(l0, __fadd_rn(a0, b0));
-          l1 = __fadd_rn(l1, __fadd_rn(a1, b1));
+          tm_st32(ts, pk);
+          tm_st32(ts + 32, pk + 32);
+          l0 = __fadd_rn(l0, a0);
+          l1 = __fadd_rn(l1, a1);
           tm_wait_st();
         }
         if (t == nt - 1 && (!wide || s == 0) && ends) {
@@ -848,12 +903,12 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
           uint32_t o[32];
           float y[32];
           tm_ld32(o, tmem + lanes + 256 + (wide ? s * D : 0) + c);
-          tm_wait_ld();
+          tm_wait_ld(o);
 #pragma unroll
           for (int k = 0; k < 32; k++) y[k] = f0 == 0.0f ? 0.0f : __fmul_rn(__uint_as_float(o[k]), f0);
           if (!wide && nt > 1) {
             tm_ld32(o, tmem + lanes + 256 + D + c);
-            tm_wait_ld();
+            tm_wait_ld(o);
 #pragma unroll
             for (int k = 0; k < 32; k++) y[k] = f1 == 0.0f ? y[k] : fmaf(__uint_as_float(o[k]), f1, y[k]);
           }
