@@ -28,7 +28,9 @@ namespace rs {
 namespace {
 
 constexpr int TK = 128;        // keys of a tile
-constexpr int OV = 1;          // a job's own cost in tiles: its rows' loads and stores
+// Costs: a tile of a job of at most 128 rows, one of a larger job, and a job's
+// own (its rows' loads and stores).
+constexpr int W_NARROW = 2, W_WIDE = 3, OV = 2;
 constexpr int NT_PLAN = 1024;
 constexpr int NT_ATT = 384;
 constexpr int PLAN_GROUPS = 1024;   // groups whose sums are kept in shared memory
@@ -37,6 +39,7 @@ constexpr int PLAN_JOBS = 4096;     // jobs whose costs are
 constexpr int JOB_ALONE = 1;   // no other job has its rows
 constexpr int JOB_EVEN = 2;    // every row sees all the job's keys
 constexpr int JOB_PREFIX = 4;  // a group's prefix
+constexpr int JOB_WIDE = 8;    // more than 128 rows
 
 }  // namespace
 
@@ -52,7 +55,7 @@ struct __align__(16) KvJob {
 
 struct KvHead {
   int64_t total, per;   // cost of all jobs and heads, of one CTA
-  int32_t jobs, reserved0;
+  int32_t jobs, prefix_jobs;
 };
 
 struct KvStart {
@@ -62,9 +65,6 @@ struct KvStart {
 // Jobs of a request's rows.
 struct KvReq {
   int32_t job0;    // its first own job
-  int32_t pjob0;   // first job of its group's prefix, or -1
-  int32_t ptok0;   // first row of the group
-  int32_t reserved0;
 };
 
 struct KvPlan {
@@ -145,6 +145,14 @@ __device__ __forceinline__ int prefix_keys(const rs_kv_batch& b, int g) {
 
 __device__ __forceinline__ int tiles(int keys) { return keys > 0 ? (keys + TK - 1) / TK : 0; }
 
+__device__ __forceinline__ int tile_cost(int flags) { return (flags & JOB_WIDE) ? W_WIDE : W_NARROW; }
+// (a job without keys whose rows nobody else has writes their zeros)
+__device__ __forceinline__ int job_cost(int nt, int flags) {
+  return nt > 0 ? nt * tile_cost(flags) + OV : (flags & JOB_ALONE) ? OV : 0;
+}
+// The first tile that starts at cost `off` of a job or after it.
+__device__ __forceinline__ int tile_at(int off, int w) { return off <= OV ? 0 : (off - OV + w - 1) / w; }
+
 // One CTA: whether each group's prefix pays as one job for all its rows, the
 // jobs, their costs' sums, and every CTA's start.  Latency is all that counts
 // here (a few dependent reads and block sums); sums live in shared memory at
@@ -171,8 +179,9 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
       if (g < 0 || r.q == 0) continue;
       const int P = prefix_keys(b, g), rt = (r.q + w2 - 1) / w2, seen = r.kv - (r.q >> 1);
       const int t = tiles(seen), ts = tiles(seen - P);
-      atomicAdd(&sum[4 * g], (unsigned long long)rt * (t ? t + OV : 0));
-      atomicAdd(&sum[4 * g + 1], (unsigned long long)rt * (ts ? ts + OV : 0));
+      const int fl = r.q > p.tpt ? JOB_WIDE : 0;
+      atomicAdd(&sum[4 * g], (unsigned long long)rt * job_cost(t, fl));
+      atomicAdd(&sum[4 * g + 1], (unsigned long long)rt * job_cost(ts, fl));
       if (r.kv - r.q + 1 < P) sum[4 * g + 2] = 1;
       atomicMax(&sum[4 * g + 3], (unsigned long long)r.kv);
     }
@@ -194,8 +203,8 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
       t1 = clampi(b.q_start[max(first, last)], 0, b.n_tokens);
       const int rt = t1 > t0 ? (t1 - t0 + w2 - 1) / w2 : 0;
       P = (int)min((unsigned long long)P, of(4 * g + 3));   // (a prefix that nobody has written yet is not read)
-      const unsigned long long with = of(4 * g + 1) + (unsigned long long)rt * (tiles(P) + OV) +
-                                      (unsigned long long)(max(t1 - t0, 0) >> 2);
+      const unsigned long long with = of(4 * g + 1) + (unsigned long long)rt * job_cost(tiles(P), t1 - t0 > p.tpt ? JOB_WIDE : 0) +
+                                      (unsigned long long)(max(t1 - t0, 0) >> 1);
       if (P > 0 && first < last && with < of(4 * g)) cnt = rt;
     }
     const int64_t at = jobs + block_scan(cnt, s_scan, &total);
@@ -217,24 +226,24 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
         j.kend = P;
         j.nt = tiles(P);
         j.lim0 = P;
-        j.flags = JOB_PREFIX | (even ? JOB_EVEN : 0);
+        j.flags = JOB_PREFIX | (even ? JOB_EVEN : 0) | (j.ntok > p.tpt ? JOB_WIDE : 0);
         p.jobs[at + k] = j;
       }
     }
   }
   jobs = min(jobs, (int64_t)p.cap);
+  const int prefix_jobs = (int)jobs;
   __syncthreads();   // gjob
   // the requests' own jobs
   for (int base = 0; base < n; base += NT_PLAN) {
     const int i = base + tid;
     ReqLens r{0, 0, 0};
-    int key0 = 0, cnt = 0, pj = -1, pt = 0;
+    int key0 = 0, cnt = 0, pj = -1;
     if (i < n) {
       r = kv_req(b, i);
       const int g = group_of(b, i);
       if (g >= 0 && p.gjob[g] >= 0) {
         pj = p.gjob[g];
-        pt = clampi(b.q_start[clampi(b.group_start[g], 0, n)], 0, b.n_tokens);
         key0 = prefix_keys(b, g);
       }
       cnt = (r.q + w2 - 1) / w2;
@@ -242,7 +251,7 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
     const int64_t at = jobs + block_scan(cnt, s_scan, &total);
     jobs += total;
     const bool fits = cnt > 0 && at + cnt <= p.cap;
-    if (i < n) p.req[i] = KvReq{fits ? (int32_t)at : -1, pj, pt, 0};
+    if (i < n) p.req[i] = KvReq{fits ? (int32_t)at : -1};
     // a request of one job is its thread's; a longer one is its warp's
     for (int k = 0; !fits && k < cnt && at + k < p.cap; k++) p.jobs[at + k] = KvJob{};   // (as above)
     unsigned todo = __ballot_sync(~0u, fits);
@@ -258,7 +267,7 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
       j.kend = clampi((int64_t)kv - q + e, 0, (int)min((int64_t)b.max_blocks * 16, (int64_t)INT_MAX - 256));
       j.nt = tiles(j.kend - key0);
       j.lim0 = kv - q + a + 1;
-      j.flags = pj < 0 ? JOB_ALONE : 0;
+      j.flags = (pj < 0 ? JOB_ALONE : 0) | (j.ntok > p.tpt ? JOB_WIDE : 0);
       p.jobs[at + k] = j;
     };
     if (lone & mine) put(at, 0, i, r.q0, r.q, r.kv, key0, pj);
@@ -274,16 +283,23 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
       for (int k = tid & 31; k < sc; k += 32) put(sat, k, si, s0, sq, sk, s1, sp);
     }
   }
-  const int J = (int)min(jobs, (int64_t)p.cap);
+  // rows of no request: jobs without keys
+  const int q_end = n > 0 ? clampi(b.q_start[n], 0, b.n_tokens) : 0;
+  const int pads = (b.n_tokens - q_end + w2 - 1) / w2;
+  for (int k = tid; k < pads && jobs + k < p.cap; k += NT_PLAN) {
+    KvJob j = {};
+    j.tok0 = q_end + k * w2;
+    j.ntok = min(w2, b.n_tokens - j.tok0);
+    j.flags = JOB_ALONE | (j.ntok > p.tpt ? JOB_WIDE : 0);
+    p.jobs[jobs + k] = j;
+  }
+  const int J = (int)min(jobs + pads, (int64_t)p.cap);
   __syncthreads();   // the jobs
   int64_t cost = 0;
   for (int base = 0; base <= J; base += NT_PLAN) {
     const int j = base + tid;
     int64_t c = 0;
-    if (j < J) {
-      const int nt = p.jobs[j].nt;
-      c = nt > 0 ? nt + OV : 0;
-    }
+    if (j < J) c = job_cost(p.jobs[j].nt, p.jobs[j].flags);
     const int64_t at = cost + block_scan(c, s_scan, &total);
     cost += total;
     if (j <= J) {
@@ -294,8 +310,8 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
   __syncthreads();
   const int64_t all = cost * n_kv_heads;
   // two tiles at least, one for each stream of a CTA
-  const int64_t per = max((all + p.ctas - 1) / p.ctas, (int64_t)(2 + OV));
-  if (tid == 0) *p.head = KvHead{all, per, J, 0};
+  const int64_t per = max((all + p.ctas - 1) / p.ctas, (int64_t)(2 * W_NARROW + OV));
+  if (tid == 0) *p.head = KvHead{all, per, J, prefix_jobs};
   const int64_t* cs = J <= PLAN_JOBS ? s_cost : p.cost;
   for (int c = tid; c < p.ctas; c += NT_PLAN) {
     const int64_t u = c * per;
@@ -501,16 +517,40 @@ __device__ __forceinline__ void row_exp(uint32_t ts, bool cut, int left, float s
 
 // ------------------------------------------------------------------ the kernel
 
-// A CTA's share of the jobs: next() gives the segments (a job and head's tiles
-// t0 .. t1 - 1) in order.  Every role of the CTA walks it by itself.
+// Tiles t0 .. t1 - 1 of a job and head.
+struct Seg {
+  KvJob job;
+  int head, t0, t1;
+  int cut_front;        // the CTA's share began inside the job
+  __device__ bool wide() const { return job.flags & JOB_WIDE; }
+  __device__ int nt() const { return t1 - t0; }
+};
+
+// What a CTA's two streams do together, in shared memory for its warps:
+//   RUN_WIDE   one job of more than 128 rows, half of them each
+//   RUN_SPLIT  one job of fewer rows, every other tile each, joined at the end
+//   RUN_PAIR   two such jobs, one each (short ones: no join, and one stream's stores
+//              run under the other's products)
+//   RUN_NONE   rows without keys
+//   RUN_END    no more
+enum { RUN_WIDE, RUN_SPLIT, RUN_PAIR, RUN_NONE, RUN_END };
+
+struct Run {
+  Seg seg[2];           // of stream 0 (or both), of stream 1 in a RUN_PAIR
+  int kind, n[2];       // tiles of each stream
+  int reserved0;
+  int32_t page[32];     // blocks of each stream's first two tiles
+};
+
+// A CTA's share of the jobs, as runs.
 struct Walk {
   const KvJob* jobs;
   int64_t rem;
   int j, h, off, heads;
-  KvJob job;            // of the segment given last
-  int head, t0, t1;
-  bool cut_front;       // the share began inside the job
   KvJob ahead;          // job j
+  bool held;            // b waits for its turn
+  int kind;
+  Seg a, b;
 
   __device__ Walk(const KvPlan& p, int n_kv_heads) {
     const KvHead hd = *p.head;
@@ -520,21 +560,23 @@ struct Walk {
     rem = min(hd.per, hd.total - u);
     const KvStart s = p.start[blockIdx.x];
     j = s.job; h = s.head; off = s.off;
+    held = false;
     if (rem > 0) ahead = jobs[j];
   }
-  __device__ bool next() {
+  __device__ bool pull(Seg& s) {
     while (rem > 0) {
-      const int cost = ahead.nt > 0 ? ahead.nt + OV : 0;
+      const int cost = job_cost(ahead.nt, ahead.flags);
       if (cost == 0) {
         ahead = jobs[++j];
         continue;
       }
-      const int take = (int)min((int64_t)(cost - off), rem);
-      t0 = max(off - OV, 0);
-      t1 = max(off + take - OV, 0);
-      cut_front = off > 0;
-      head = h;
-      job = ahead;
+      const int take = (int)min((int64_t)(cost - off), rem), w = tile_cost(ahead.flags);
+      const bool empty = ahead.nt == 0 && off == 0;
+      s.t0 = min(tile_at(off, w), ahead.nt);
+      s.t1 = min(tile_at(off + take, w), ahead.nt);
+      s.cut_front = off > 0;
+      s.head = h;
+      s.job = ahead;
       rem -= take;
       off += take;
       if (off == cost) {
@@ -545,9 +587,31 @@ struct Walk {
           if (rem > 0) ahead = jobs[j];
         }
       }
-      if (t1 > t0) return true;
+      if (s.t1 > s.t0 || empty) return true;
     }
     return false;
+  }
+  __device__ void next() {
+    if (held) {
+      a = b;
+    } else if (!pull(a)) {
+      kind = RUN_END;
+      return;
+    }
+    held = false;
+    if (a.nt() == 0) {
+      kind = RUN_NONE;
+    } else if (a.wide()) {
+      kind = RUN_WIDE;
+    } else {
+      kind = RUN_SPLIT;
+      held = pull(b);
+      // streams of much the same length
+      if (held && !b.wide() && b.nt() > 0 && 2 * b.nt() >= a.nt() && 2 * a.nt() >= b.nt()) {
+        kind = RUN_PAIR;
+        held = false;
+      }
+    }
   }
 };
 
@@ -558,22 +622,24 @@ struct Lay {
   static constexpr int NST = D == 128 ? 5 : 12;   // stages: what 227 KB leave beside the rows
   static constexpr int RING = 2 * QSLOT;
   static constexpr int MISC = RING + NST * STAGE;
-  // barriers: full[NST], empty[NST], qfull[2], qempty[2], sfull[2], pfull[2], ofull[2], oempty
-  static constexpr int NBAR = 2 * NST + 11;
-  static constexpr int ML = MISC + 512;           // float2 [2][128]
-  static constexpr int SMEM = ML + 2048;
+  // barriers: full[NST], empty[NST], qfull[2], qempty[2], sfull[2], pfull[2], ofull[2], oempty[2], rfull[2], rempty[2], meet
+  static constexpr int NBAR = 2 * NST + 17;
+  static constexpr int ML = MISC + 384;           // float2 [2][128]
+  static constexpr int RUNS = ML + 2048;          // Run [2]
+  static constexpr int SMEM = RUNS + 2 * (int)sizeof(Run);
 };
 
-// Place of K tile t and V tile t of a segment of n tiles in its loads' order
-// K0 K1 V0 K2 V1 ... (the order in which they are first used)
-__device__ __forceinline__ int kplace(int t) { return t == 0 ? 0 : 2 * t - 1; }
-__device__ __forceinline__ int vplace(int t, int n) { return min(2 * t + 2, 2 * n - 1); }
+// The loads' order is that of first use: K of each stream's first tile, then for
+// i = 0, 1, ... and each stream the V of its tile i and the K of its tile i + 1
+// (a RUN_WIDE job's streams share the tiles: those of stream 0).  The loads before
+// the V of stream s's tile i:
+__device__ __forceinline__ int vplace(int s, int i, int n0, int n1) {
+  auto upto = [&](int n) { return min(i, n) + min(i, max(n - 1, 0)); };
+  return (n0 > 0) + (n1 > 0) + upto(n0) + upto(n1) + (s ? (i < n0) + (i + 1 < n0) : 0);
+}
 
 // Two streams of 128 rows share the tensor cores, so that one's softmax runs
-// under the other's products.  Of a job of more than 128 rows each stream has
-// half, both over every tile; a job of fewer rows is one Q for both streams,
-// which take every other tile each and are joined at the end.  Warps 0-3
-// and 4-7 are the streams' softmax, a thread a row; warp 8 issues the products and
+// under the other's products.  Warps 0-3 and 4-7 are the streams' softmax, a thread a row; warp 8 issues the products and
 // warp 9 the loads.
 // TMEM: S of each stream 128 columns (P, 64 columns, overwrites it), O D each.
 // The m of a row is the largest score of its first tile and moves only when a
@@ -590,10 +656,12 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
   const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;
   const uint32_t bars = base + L::MISC;
   const uint32_t FULL = bars, EMPTY = bars + 8 * L::NST, QFULL = bars + 16 * L::NST, QEMPTY = QFULL + 16,
-                 SFULL = QFULL + 32, PFULL = QFULL + 48, OFULL = QFULL + 64, OEMPTY = QFULL + 80;
+                 SFULL = QFULL + 32, PFULL = QFULL + 48, OFULL = QFULL + 64, OEMPTY = QFULL + 80,
+                 RFULL = QFULL + 96, REMPTY = QFULL + 112, MEET = QFULL + 128;
+  Run* const runs = reinterpret_cast<Run*>(sm + L::RUNS);
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(sm + L::MISC + 8 * L::NBAR);
   volatile int* lost = reinterpret_cast<volatile int*>(sm + L::MISC + 8 * L::NBAR + 4);
-  static_assert(8 * L::NBAR + 8 <= 512, "barriers");
+  static_assert(8 * L::NBAR + 8 <= 384, "barriers");
   static_assert(L::SMEM <= 227 * 1024, "shared memory");
   if (base & 1023) {   // (swizzled tiles lie on 1024-byte boundaries)
     if (tid == 0) *reinterpret_cast<volatile int32_t*>(p.err) = 1;
@@ -607,8 +675,11 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
       mbar_init(SFULL + 8 * s, 1);
       mbar_init(PFULL + 8 * s, 4);
       mbar_init(OFULL + 8 * s, 1);
+      mbar_init(OEMPTY + 8 * s, 4);
+      mbar_init(RFULL + 8 * s, 1);
+      mbar_init(REMPTY + 8 * s, 10);
     }
-    mbar_init(OEMPTY, 8);
+    mbar_init(MEET, 8);
     *lost = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -626,73 +697,111 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-    Walk w(p, a.c.n_kv_heads);
-    uint32_t loads = 0;   // tiles loaded before this segment
-    if (warp == 9) {
-      // ---------------- loads
-      uint32_t qn = 0;    // Q slots used before this segment
-      auto stage_wait = [&](uint32_t x) {   // until load x's stage is free
-        const uint32_t use = x / L::NST;
-        if (use > 0) mbar_wait(EMPTY + 8 * (x % L::NST), (use - 1) & 1, lost, p.err);
-      };
-      while (w.next() && !*lost) {
-        const bool wide = w.job.ntok > p.tpt;
-        const int nt = w.t1 - w.t0;
-        const int32_t* table = a.b.table + (int64_t)w.job.row * a.b.table_stride;
-        const int page0 = w.job.key0 / 16 + w.t0 * (TK / 16), pend = (w.job.kend + 15) / 16;
-        // a lane's entry of the next 32 pages (four tiles), for K and, one tile behind, V
-        int kb = 0, ids = 0, prev_ids = 0;
-        auto fetch = [&](int t) {
-          if (t >= nt) return;
-          prev_ids = ids;
-          kb = t;
-          const int pg = page0 + t * (TK / 16) + lane;
-          int id = pg < pend ? table[pg] : 0;
-          if (id < 0 || id >= a.c.n_blocks) id = (int)a.c.n_blocks;   // reads as zeros
-          ids = id;
-        };
-        auto tile = [&](int t, bool v, uint32_t x) {
-          const int from = (t & ~3) == kb ? ids : prev_ids;
-          const int id = __shfl_sync(~0u, from, (t & 3) * 8 + (lane & 7));
-          const int pages = min(TK / 16, pend - page0 - t * (TK / 16));
-          const uint32_t bar = FULL + 8 * (x % L::NST);
-          const uint32_t dst = base + L::RING + (x % L::NST) * L::STAGE;
-          stage_wait(x);
-          if (lane == 0) mbar_expect(bar, pages * 16 * D * 2);
-          __syncwarp();
-          if (lane < pages) {
+    if (warp == 10) {
+      // ---------------- runs
+      Walk w(p, a.c.n_kv_heads);
+      for (uint32_t k = 0; !*lost; k++) {
+        w.next();
+        // the lane's page: stream lane / 16, its tile (lane / 8) % 2
+        const int s = lane >> 4, i = (lane >> 3) & 1;
+        const Seg& g = w.kind == RUN_PAIR && s ? w.b : w.a;
+        const int t = g.t0 + (w.kind == RUN_SPLIT ? 2 * i + s : i), pg = g.job.key0 / 16 + t * (TK / 16) + (lane & 7);
+        int id = 0;
+        if (w.kind <= RUN_PAIR && t < g.t1 && pg < (g.job.kend + 15) / 16)
+          id = a.b.table[(int64_t)g.job.row * a.b.table_stride + pg];
+        if (id < 0 || id >= a.c.n_blocks) id = (int)a.c.n_blocks;   // reads as zeros
+        if (k >= 2) mbar_wait(REMPTY + 8 * (k & 1), ((k >> 1) - 1) & 1, lost, p.err);
+        Run* const r = runs + (k & 1);
+        r->page[lane] = id;
+        if (lane == 0) {
+          const int n = w.a.nt();
+          r->seg[0] = w.a;
+          r->seg[1] = w.b;
+          r->kind = w.kind;
+          r->n[0] = w.kind == RUN_SPLIT ? (n + 1) >> 1 : n;
+          r->n[1] = w.kind == RUN_SPLIT ? n >> 1 : w.kind == RUN_PAIR ? w.b.nt() : n;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(RFULL + 8 * (k & 1));
+        if (w.kind == RUN_END) break;
+      }
+    } else if (warp == 9) {
+      // ---------------- loads (the warp as one; one thread issues)
+      uint32_t qn = 0, x = 0;   // Q slots used, tiles loaded
+      for (uint32_t k = 0; !*lost; k++) {
+        mbar_wait(RFULL + 8 * (k & 1), (k >> 1) & 1, lost, p.err);
+        const Run& r = runs[k & 1];
+        const int kind = r.kind;
+        if (kind == RUN_END) break;
+        if (kind != RUN_NONE) {
+          const int n0 = r.n[0], n1 = kind == RUN_WIDE ? 0 : r.n[1];
+          const bool split = kind == RUN_SPLIT;
+          // the lane's page of two tiles of its stream (lanes 16 to 31: stream 1), now, next and before
+          const Seg& g = r.seg[kind == RUN_PAIR ? lane >> 4 : 0];
+          const int32_t* pages = a.b.table + (int64_t)g.job.row * a.b.table_stride;
+          const int p0 = g.job.key0 / 16 + (lane & 7), pend = (g.job.kend + 15) / 16;
+          auto fetch = [&](int pair) {
+            const int i = 2 * pair + ((lane >> 3) & 1), t = g.t0 + (split ? 2 * i + (lane >> 4) : i);
+            const int pg = p0 + t * (TK / 16);
+            int id = t < g.t1 && pg < pend ? pages[pg] : 0;
+            return id < 0 || id >= a.c.n_blocks ? (int)a.c.n_blocks : id;
+          };
+          int now = r.page[lane], ahead = fetch(1), old = 0, at = 0;
+          for (int u = 1; u < 4 * (max(n0, n1) + 1); u++) {
+            // V of tile u / 4 - 1, K of the tile after it
+            const int s = (u >> 1) & 1, i = (u >> 2) - 1 + (u & 1);
+            const bool v = !(u & 1);
+            if (i < 0 || i >= (s ? n1 : n0)) continue;
+            if ((i >> 1) > at) {
+              at++;
+              old = now;
+              now = ahead;
+              ahead = fetch(at + 1);
+            }
+            const int from = (i >> 1) == at ? now : old;
+            const Seg& gs = r.seg[kind == RUN_PAIR ? s : 0];
+            const int t = gs.t0 + (split ? 2 * i + s : i);
+            const int cnt = min(TK / 16, (gs.job.kend + 15 - gs.job.key0) / 16 - t * (TK / 16));
+            const uint32_t st = x % L::NST, use = x / L::NST;
+            const uint32_t bar = FULL + 8 * st, dst = base + L::RING + st * L::STAGE;
+            int id[TK / 16];
 #pragma unroll
-            for (int hf = 0; hf < D / 64; hf++)
-              tma_4d(dst + hf * (TK * 128) + lane * 2048, v ? &mv : &mk, hf * 64, 0, w.head, id, bar);
+            for (int q = 0; q < TK / 16; q++) id[q] = __shfl_sync(~0u, from, s * 16 + (i & 1) * 8 + q);
+            if (use > 0) mbar_wait(EMPTY + 8 * st, (use - 1) & 1, lost, p.err);
+            const int head = gs.head;
+            if (elect_one()) {
+              const CUtensorMap* m = v ? &mv : &mk;
+              mbar_expect(bar, cnt * 16 * D * 2);
+#pragma unroll
+              for (int q = 0; q < TK / 16; q++)
+                if (q < cnt)
+#pragma unroll
+                  for (int hf = 0; hf < D / 64; hf++)
+                    tma_4d(dst + hf * (TK * 128) + q * 2048, m, hf * 64, 0, head, id[q], bar);
+            }
+            __syncwarp();
+            x++;
+            if (u == 1 || (u == 3 && kind == RUN_PAIR)) {   // the rows, after the first K
+              for (int o = 0; o < (kind == RUN_WIDE ? 2 : 1); o++) {
+                const uint32_t slot = qn & 1, quse = qn >> 1;
+                if (quse > 0) mbar_wait(QEMPTY + 8 * slot, (quse - 1) & 1, lost, p.err);
+                const bool one = gs.job.ntok == 1;
+                const int tok = gs.job.tok0 + o * p.tpt;
+                if (elect_one()) {
+                  const uint32_t qbar = QFULL + 8 * slot;
+                  mbar_expect(qbar, (one ? 1 : p.tpt) * p.ratio * D * 2);
+#pragma unroll
+                  for (int hf = 0; hf < D / 64; hf++)
+                    tma_3d(base + slot * L::QSLOT + hf * (128 * 128), one ? &mq1 : &mq, hf * 64, head * p.ratio, tok, qbar);
+                }
+                __syncwarp();
+                qn++;
+              }
+            }
           }
-          __syncwarp();
-        };
-        fetch(0);
-        tile(0, false, loads);
-        // the rows, into one slot or two
-        for (int s = 0; s < (wide ? 2 : 1); s++) {
-          const uint32_t slot = (qn + s) & 1, use = (qn + s) >> 1;
-          if (use > 0) mbar_wait(QEMPTY + 8 * slot, (use - 1) & 1, lost, p.err);
-          if (lane == 0) {
-            const bool one = w.job.ntok == 1;
-            const uint32_t bar = QFULL + 8 * slot;
-            mbar_expect(bar, (one ? 1 : p.tpt) * p.ratio * D * 2);
-            for (int hf = 0; hf < D / 64; hf++)
-              tma_3d(base + slot * L::QSLOT + hf * (128 * 128), one ? &mq1 : &mq, hf * 64, w.head * p.ratio,
-                     w.job.tok0 + s * p.tpt, bar);
-          }
-          __syncwarp();
         }
-        qn += wide ? 2 : 1;
-        if (nt > 1) tile(1, false, loads + 1);
-        for (int t = 0; t < nt; t++) {
-          tile(t, true, loads + vplace(t, nt));
-          if (t + 2 < nt) {
-            if (((t + 2) & 3) == 0) fetch(t + 2);
-            tile(t + 2, false, loads + kplace(t + 2));
-          }
-        }
-        loads += 2 * nt;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(REMPTY + 8 * (k & 1));
       }
     } else if (warp == 8) {
       // ---------------- products (the warp as one; one thread issues)
@@ -701,54 +810,65 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
       constexpr uint32_t IPV = (1u << 4) | (FMT << 7) | (FMT << 10) | (1u << 16) | ((D / 8) << 17) | ((128 / 16) << 24);
       const uint64_t dq = smem_desc(base, 16), dk = smem_desc(base + L::RING, 16),
                      dv = smem_desc(base + L::RING, TK * 128);
-      uint32_t qn = 0, np[2] = {0, 0}, segs = 0;
-      while (w.next() && !*lost) {
-        const bool wide = w.job.ntok > p.tpt;
-        const int nt = w.t1 - w.t0, E = wide ? 2 * nt : nt;
-        auto qk = [&](int e) {
-          const uint32_t s = e & 1, t = wide ? e >> 1 : e;
-          const uint32_t x = loads + kplace(t), slot = (qn + (wide ? s : 0)) & 1, st = x % L::NST;
-          if (!wide || s == 0) mbar_wait(FULL + 8 * st, (x / L::NST) & 1, lost, p.err);
-          if (t == 0) mbar_wait(QFULL + 8 * slot, ((qn + (wide ? s : 0)) >> 1) & 1, lost, p.err);
-          tc_after();
-          const uint64_t qa = dq + slot * (L::QSLOT >> 4), ka = dk + st * (L::STAGE >> 4);
-          if (elect_one()) {
+      uint32_t x = 0, qn = 0, np0 = 0, np1 = 0, done = 0;
+      uint32_t kst = 0, vst = 0;   // stages of the last K and V tile
+      auto take = [&]() {   // the next load's stage
+        const uint32_t st = x % L::NST;
+        mbar_wait(FULL + 8 * st, (x / L::NST) & 1, lost, p.err);
+        x++;
+        return st;
+      };
+      for (uint32_t k = 0; !*lost; k++) {
+        mbar_wait(RFULL + 8 * (k & 1), (k >> 1) & 1, lost, p.err);
+        const int kind = runs[k & 1].kind, n0 = runs[k & 1].n[0], n1 = runs[k & 1].n[1];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(REMPTY + 8 * (k & 1));
+        if (kind == RUN_END) break;
+        if (kind == RUN_NONE) continue;
+        const bool wide = kind == RUN_WIDE, split = kind == RUN_SPLIT;
+        for (int u = 0; u < 2 * (max(n0, n1) + 1); u++) {
+          const uint32_t s = u & 1;
+          const int i = (u >> 1) - 1, n = s ? n1 : n0;
+          if (i >= 0 && i < n) {   // O += P V of tile i
+            if (!wide || s == 0) vst = take();
+            if (i == 0 && done > 0) mbar_wait(OEMPTY + 8 * s, (done - 1) & 1, lost, p.err);
+            mbar_wait(PFULL + 8 * s, (s ? np1 : np0) & 1, lost, p.err);
+            np0 += s == 0;
+            np1 += s == 1;
+            tc_after();
+            const uint64_t va = dv + vst * (L::STAGE >> 4);
+            const uint32_t more = i > 0;   // O holds something
+            if (elect_one()) {
 #pragma unroll
-            for (int k = 0; k < D / 16; k++) {
-              const uint32_t o = ((k >> 2) * (128 * 128) + (k & 3) * 32) >> 4;
-              mma_ss(tmem + s * 128, qa + o, ka + o, IQK, k > 0);
+              for (int q = 0; q < TK / 16; q++)
+                mma_ts(tmem + 256 + s * D, tmem + s * 128 + q * 8, va + q * (2048 >> 4), IPV, q > 0 ? 1u : more);
+              if (!wide || s == 1) mma_commit(EMPTY + 8 * vst);
+              if (i + 1 == n) mma_commit(OFULL + 8 * s);
             }
-            mma_commit(SFULL + 8 * s);
-            if (!wide || s == 1) mma_commit(EMPTY + 8 * st);
-            if (t == nt - 1) mma_commit(QEMPTY + 8 * slot);
+            __syncwarp();
           }
-          __syncwarp();
-        };
-        qk(0);
-        if (E > 1) qk(1);
-        for (int e = 0; e < E; e++) {
-          const uint32_t s = e & 1, t = wide ? e >> 1 : e;
-          const uint32_t x = loads + vplace(t, nt), st = x % L::NST;
-          if (!wide || s == 0) mbar_wait(FULL + 8 * st, (x / L::NST) & 1, lost, p.err);
-          if (e == 0 && segs > 0) mbar_wait(OEMPTY, (segs - 1) & 1, lost, p.err);
-          mbar_wait(PFULL + 8 * s, (s ? np[1] : np[0]) & 1, lost, p.err);
-          if (s) np[1]++; else np[0]++;
-          tc_after();
-          const uint64_t va = dv + st * (L::STAGE >> 4);
-          const uint32_t more = wide ? t > 0 : e >= 2;   // O holds something
-          if (elect_one()) {
+          if (i + 1 < n) {   // S = Q K^T of tile i + 1
+            if (!wide || s == 0) kst = take();
+            const uint32_t qi = qn + (split ? 0 : s), slot = qi & 1;
+            if (i < 0 && !(split && s)) mbar_wait(QFULL + 8 * slot, (qi >> 1) & 1, lost, p.err);
+            tc_after();
+            const uint64_t qa = dq + slot * (L::QSLOT >> 4), ka = dk + kst * (L::STAGE >> 4);
+            const bool end = split ? 2 * (i + 1) + (int)s + 1 == n0 + n1 : i + 2 == n;
+            if (elect_one()) {
 #pragma unroll
-            for (int k = 0; k < TK / 16; k++)
-              mma_ts(tmem + 256 + s * D, tmem + s * 128 + k * 8, va + k * (2048 >> 4), IPV, k > 0 ? 1u : more);
-            if (!wide || s == 1) mma_commit(EMPTY + 8 * st);
-            if (e + 2 >= E) mma_commit(OFULL + 8 * s);
+              for (int q = 0; q < D / 16; q++) {
+                const uint32_t o = ((q >> 2) * (128 * 128) + (q & 3) * 32) >> 4;
+                mma_ss(tmem + s * 128, qa + o, ka + o, IQK, q > 0);
+              }
+              mma_commit(SFULL + 8 * s);
+              if (!wide || s == 1) mma_commit(EMPTY + 8 * kst);
+              if (end) mma_commit(QEMPTY + 8 * slot);
+            }
+            __syncwarp();
           }
-          __syncwarp();
-          if (e + 2 < E) qk(e + 2);
         }
-        qn += wide ? 2 : 1;
-        segs++;
-        loads += 2 * nt;
+        qn += split ? 1 : 2;
+        done++;
       }
     }
   } else {
@@ -759,46 +879,69 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
     const uint32_t ts = tmem + lanes + s * 128;
     const float sl = __fmul_rn(a.scale, 1.4426950408889634f);
     float2* ml = reinterpret_cast<float2*>(sm + L::ML);
-    uint32_t ns = 0, no[2] = {0, 0}, loads = 0;
-    Walk w(p, a.c.n_kv_heads);
+    uint32_t ns = 0, no0 = 0, no1 = 0, loads = 0;
     const int tl = r / p.ratio, hl = r - tl * p.ratio;   // the row's token and head in its 128
-    while (w.next()) {   // (both streams meet in here: neither leaves early)
-      const bool wide = w.job.ntok > p.tpt;
-      const int nt = w.t1 - w.t0;
-      const int tok = (wide ? s * p.tpt : 0) + tl;
-      const bool live = tl < p.tpt && tok < w.job.ntok;
+    const int64_t all = (int64_t)a.b.n_tokens * a.n_heads;
+    uint32_t nm = 0;
+    auto meet = [&]() {   // of both streams' warps
+      __syncwarp();
+      if (lane == 0) mbar_arrive(MEET);
+      mbar_wait(MEET, nm++ & 1, lost, p.err);
+    };
+    for (uint32_t k = 0;; k++) {
+      mbar_wait(RFULL + 8 * (k & 1), (k >> 1) & 1, lost, p.err);
+      const Run& run = runs[k & 1];
+      const int kind = run.kind;
+      if (kind == RUN_END || *lost) break;
+      const bool wide = kind == RUN_WIDE, split = kind == RUN_SPLIT;
+      const Seg& g = run.seg[kind == RUN_PAIR ? s : 0];
+      const KvJob& job = g.job;
+      const int tok = ((job.flags & JOB_WIDE) && s ? p.tpt : 0) + tl;
+      const bool live = tl < p.tpt && tok < job.ntok;
+      const int row = job.tok0 + tok, hq = g.head * p.ratio + hl;
+      if (kind == RUN_NONE) {
+        if (live && (s == 0 || (job.flags & JOB_WIDE))) {
+          uint16_t* out = static_cast<uint16_t*>(a.out) + row * a.o_ts + hq * a.o_hs;
+          for (int c = 0; c < D; c += 8) *reinterpret_cast<uint4*>(out + c) = make_uint4(0, 0, 0, 0);
+          if (a.lse) a.lse[(int64_t)row * a.n_heads + hq] = -INFINITY;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(REMPTY + 8 * (k & 1));
+        continue;
+      }
+      const int n0 = run.n[0], n1 = run.n[1], n = s ? n1 : n0;
       const bool any = __any_sync(~0u, live);
       int lim = 0;   // keys from key0 on that the row sees
       if (live) {
-        if (w.job.flags & JOB_EVEN) {
-          lim = w.job.kend;
-        } else if (w.job.flags & JOB_PREFIX) {
-          const int row = w.job.tok0 + tok;
-          int lo = w.job.row, hi = a.b.n_req;
+        if (job.flags & JOB_EVEN) {
+          lim = job.kend;
+        } else if (job.flags & JOB_PREFIX) {
+          int lo = job.row, hi = a.b.n_req;
           while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
             if (a.b.q_start[mid] <= row) lo = mid; else hi = mid;
           }
           const int64_t x = (int64_t)max(a.b.kv_len[lo], 0) - a.b.q_start[lo + 1] + row + 1;
-          lim = (int)min((int64_t)w.job.kend, max(x, (int64_t)0));
+          lim = (int)min((int64_t)job.kend, max(x, (int64_t)0));
         } else {
-          lim = (int)min((int64_t)w.job.kend, (int64_t)w.job.lim0 + tok);
+          lim = (int)min((int64_t)job.kend, (int64_t)job.lim0 + tok);
         }
-        lim -= w.job.key0;
+        lim -= job.key0;
       }
       // keys of a last tile that the job's end cuts
-      const int ends = w.t1 == w.job.nt ? (w.job.kend - w.job.key0) & (TK - 1) : 0;
+      const int ends = g.t1 == job.nt ? (job.kend - job.key0) & (TK - 1) : 0;
       const int low = __reduce_min_sync(~0u, live ? lim : INT_MAX);
       float m = live ? -INFINITY : 0.0f, l0 = 0.0f, l1 = 0.0f;
-      for (int t = wide ? 0 : s; t < nt; t += wide ? 1 : 2) {
+      for (int i = 0; i < n; i++) {
+        const int t = split ? 2 * i + s : i;
         mbar_wait(SFULL + 8 * s, ns & 1, lost, p.err);
         ns++;
         tc_after();
         if (any) {
-          const int k0 = (w.t0 + t) * TK;
+          const int k0 = (g.t0 + t) * TK;
           const bool cut = low < k0 + TK;   // (the warp's rows see different ends)
           const int left = lim - k0;
-          const bool first = wide ? t == 0 : t < 2;   // O holds nothing yet
+          const bool first = i == 0;   // O holds nothing yet
           if (first) {
             const float x = row_max(ts, cut, left);
             if (live) m = x;
@@ -834,10 +977,10 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
           l1 = __fadd_rn(l1, a1);
           tm_wait_st();
         }
-        if (t == nt - 1 && (!wide || s == 0) && ends) {
+        if (ends && t == g.nt() - 1 && !(wide && s)) {
           // V rows past the keys' end: their weights are 0, but 0 times what lies there may be NaN.
           // (Of a wide job stream 0's product with this tile comes first.)
-          const uint32_t x = loads + vplace(t, nt);
+          const uint32_t x = loads + vplace(s, i, n0, wide ? 0 : n1);
           mbar_wait(FULL + 8 * (x % L::NST), (x / L::NST) & 1, lost, p.err);
           uint4* vt = reinterpret_cast<uint4*>(sm + L::RING + (x % L::NST) * L::STAGE);
 #pragma unroll
@@ -849,25 +992,22 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
         __syncwarp();
         if (lane == 0) mbar_arrive(PFULL + 8 * s);
       }
-      loads += 2 * nt;
+      loads += 2 * (n0 + (wide ? 0 : n1));
       // ---- the rows' results: the stream's own, or both streams' joined, half the columns each
       float l = __fadd_rn(l0, l1);
       float f0, f1 = 0.0f, lse2;
       int c0 = 0, c1 = D;
-      if (wide) {
-        f0 = l > 0.0f ? __fdiv_rn(1.0f, l) : 0.0f;
-        lse2 = l > 0.0f ? __fadd_rn(__fmul_rn(m, sl), __log2f(l)) : -INFINITY;
-        if (!(l == l)) f0 = lse2 = l;
-        mbar_wait(OFULL + 8 * s, no[s] & 1, lost, p.err);
-        no[0]++;   // (the other stream's has its turn too)
-        no[1]++;
+      if (!split) {
+        f0 = l > 0.0f ? __fdiv_rn(1.0f, l) : l == l ? 0.0f : l;
+        lse2 = l > 0.0f ? __fadd_rn(__fmul_rn(m, sl), __log2f(l)) : l == l ? -INFINITY : l;
+        mbar_wait(OFULL + 8 * s, (s ? no1 : no0) & 1, lost, p.err);
       } else {
         ml[s * 128 + r] = make_float2(m, l);
-        asm volatile("bar.sync 1, 256;" ::: "memory");
+        meet();
         const float2 x = ml[r], y = ml[128 + r];
-        const float mm = fmaxf(x.x, y.x);
+        const float mm = n1 > 0 ? fmaxf(x.x, y.x) : x.x;
         const float wx = x.x == -INFINITY ? 0.0f : ex2(__fmul_rn(__fsub_rn(x.x, mm), sl));
-        const float wy = y.x == -INFINITY ? 0.0f : ex2(__fmul_rn(__fsub_rn(y.x, mm), sl));
+        const float wy = n1 == 0 || y.x == -INFINITY ? 0.0f : ex2(__fmul_rn(__fsub_rn(y.x, mm), sl));
         l = fmaf(x.y, wx, __fmul_rn(y.y, wy));
         const float inv = l > 0.0f ? __fdiv_rn(1.0f, l) : l == l ? 0.0f : l;
         f0 = __fmul_rn(wx, inv);
@@ -875,38 +1015,33 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
         lse2 = l > 0.0f ? __fadd_rn(__fmul_rn(mm, sl), __log2f(l)) : l == l ? -INFINITY : l;
         c0 = s * (D / 2);
         c1 = c0 + D / 2;
-        mbar_wait(OFULL, no[0] & 1, lost, p.err);
-        no[0]++;
-        if (nt > 1) {
-          mbar_wait(OFULL + 8, no[1] & 1, lost, p.err);
-          no[1]++;
-        }
+        mbar_wait(OFULL, no0 & 1, lost, p.err);
+        if (n1 > 0) mbar_wait(OFULL + 8, no1 & 1, lost, p.err);
       }
+      no0 += n0 > 0;
+      no1 += n1 > 0;
       tc_after();
-      const bool whole = w.t0 == 0 && w.t1 == w.job.nt;
-      const bool direct = whole && (w.job.flags & JOB_ALONE);
+      const bool whole = g.t0 == 0 && g.t1 == job.nt;
+      const bool direct = whole && (job.flags & JOB_ALONE);
       if (any) {
-        const int64_t row = (int64_t)w.job.tok0 + tok;
-        const int hq = w.head * p.ratio + hl;
         // a part's row: with the other whole parts of all rows, or with the CTA's cut ones
-        const int64_t all = (int64_t)a.b.n_tokens * a.n_heads;
-        const int64_t at = whole ? ((w.job.flags & JOB_PREFIX) ? 0 : all) + row * a.n_heads + hq
-                                 : ((int64_t)blockIdx.x * 2 + (w.cut_front ? 0 : 1)) * 256 + (wide ? s * 128 : 0) + r;
-        float* part = (whole ? p.home : p.part) + at * D;
         uint16_t* out = static_cast<uint16_t*>(a.out) + row * a.o_ts + hq * a.o_hs;
+        const int64_t at = whole ? ((job.flags & JOB_PREFIX) ? 0 : all) + (int64_t)row * a.n_heads + hq
+                                 : ((int64_t)blockIdx.x * 2 + (g.cut_front ? 0 : 1)) * 256 + (wide ? s * 128 : 0) + r;
+        float* part = (whole ? p.home : p.part) + at * D;
         if (live && c0 == 0) {
           if (!direct) (whole ? p.home_lse : p.part_lse)[at] = lse2;
-          else if (a.lse) a.lse[row * a.n_heads + hq] = __fmul_rn(lse2, 0.6931471805599453f);
+          else if (a.lse) a.lse[(int64_t)row * a.n_heads + hq] = __fmul_rn(lse2, 0.6931471805599453f);
         }
 #pragma unroll 1
         for (int c = c0; c < c1; c += 32) {
           uint32_t o[32];
           float y[32];
-          tm_ld32(o, tmem + lanes + 256 + (wide ? s * D : 0) + c);
+          tm_ld32(o, tmem + lanes + 256 + (split ? 0 : s * D) + c);
           tm_wait_ld(o);
 #pragma unroll
           for (int k = 0; k < 32; k++) y[k] = f0 == 0.0f ? 0.0f : __fmul_rn(__uint_as_float(o[k]), f0);
-          if (!wide && nt > 1) {
+          if (split && n1 > 0) {
             tm_ld32(o, tmem + lanes + 256 + D + c);
             tm_wait_ld(o);
 #pragma unroll
@@ -928,9 +1063,12 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
         }
       }
       tc_before();
+      if (split) meet();   // ml and both O are free again
       __syncwarp();
-      if (lane == 0) mbar_arrive(OEMPTY);
-      if (!wide) asm volatile("bar.sync 1, 256;" ::: "memory");   // ml is free again
+      if (lane == 0) {
+        mbar_arrive(OEMPTY + 8 * s);
+        mbar_arrive(REMPTY + 8 * (k & 1));
+      }
     }
   }
   __syncthreads();
@@ -946,35 +1084,101 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
 
 // ------------------------------------------------------------------ joining
 
-// The tiles of job j, head h that CTA c has.
-__device__ __forceinline__ bool segment(int64_t u0, int cost, int64_t per, int64_t c, int& t0, int& t1) {
+// The tiles that CTA c has of a job and head of `cost` from u0 on.
+__device__ __forceinline__ bool segment(int64_t u0, int cost, int w, int nt, int64_t per, int64_t c, int& t0, int& t1) {
   const int64_t lo = max(c * per, u0) - u0, hi = min((c + 1) * per, u0 + cost) - u0;
-  t0 = max((int)lo - OV, 0);
-  t1 = max((int)hi - OV, 0);
+  if (lo >= hi) return false;
+  t0 = min(tile_at((int)lo, w), nt);
+  t1 = min(tile_at((int)hi, w), nt);
   return t1 > t0;
 }
 
-// A row (token, head) from the parts its jobs left, a warp for `rpw` heads of a
-// token's kv head; rows that no job covers become 0 and -inf.  Rows whose one
-// job was whole are done already.
+// Parts of one row (token, head).
+template <int D>
+struct Join {
+  static constexpr int E = D / 32;
+  float m, l, o[E];
+  __device__ Join() : m(-INFINITY), l(0.0f) {
+#pragma unroll
+    for (int e = 0; e < E; e++) o[e] = 0.0f;
+  }
+  // those of row rr of 256 of job j, head kh
+  __device__ void add(const KvPlan& p, const KvHead& hd, int j, const KvJob& job, int kh, int n_kv_heads,
+                      int64_t home, int rr, int lane) {
+    if (job.nt <= 0) return;
+    const int w = tile_cost(job.flags), cost = job_cost(job.nt, job.flags);
+    const int64_t u0 = p.cost[j] * n_kv_heads + (int64_t)kh * cost;
+    const int c0 = (int)(u0 / hd.per), c1 = min((int)((u0 + cost - 1) / hd.per), p.ctas - 1);
+    for (int c = c0; c <= c1; c++) {
+      int t0, t1;
+      if (!segment(u0, cost, w, job.nt, hd.per, c, t0, t1)) continue;
+      const bool whole = t0 == 0 && t1 == job.nt;
+      const int64_t at = whole ? home : ((int64_t)c * 2 + (c == c0 ? 1 : 0)) * 256 + rr;
+      const float s = (whole ? p.home_lse : p.part_lse)[at];
+      const float* src = (whole ? p.home : p.part) + at * D + lane * E;
+      float y[E];
+#pragma unroll
+      for (int e = 0; e < E; e++) y[e] = src[e];
+      if (s == -INFINITY) continue;
+      const float m2 = fmaxf(m, s), f = m == -INFINITY ? 0.0f : ex2(__fsub_rn(m, m2)), g = ex2(__fsub_rn(s, m2));
+      l = fmaf(l, f, g);
+#pragma unroll
+      for (int e = 0; e < E; e++) o[e] = fmaf(o[e], f, __fmul_rn(g, y[e]));
+      m = m2;
+    }
+  }
+  template <bool HALF>
+  __device__ void put(const KvAttendArgs& a, int64_t row, int hq, int lane) const {
+    const float inv = l == 0.0f ? 0.0f : __fdiv_rn(1.0f, l);
+    uint16_t* out = static_cast<uint16_t*>(a.out) + row * a.o_ts + hq * a.o_hs + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; e += 2)
+      *reinterpret_cast<uint32_t*>(out + e) = pack2<HALF>(__fmul_rn(o[e], inv), __fmul_rn(o[e + 1], inv));
+    if (a.lse && lane == 0)
+      a.lse[row * a.n_heads + hq] = l == 0.0f ? -INFINITY : __fmul_rn(__fadd_rn(m, __log2f(l)), 0.6931471805599453f);
+  }
+};
+
+// Rows that have parts, a warp a row: those of the jobs that a share's end cut
+// (first looked for at each CTA's start), and those of shared groups, which
+// have a prefix job and an own one.  The order of the parts is the keys'.
 template <int D, bool HALF>
 __global__ void __launch_bounds__(128) k_kv_join(const __grid_constant__ KvAttendArgs a,
-                                                 const __grid_constant__ KvPlan p, int rpw) {
+                                                 const __grid_constant__ KvPlan p) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  constexpr int E = D / 32;
   const int lane = threadIdx.x & 31;
-  const int units = a.n_heads / rpw;
-  const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-  if (w >= (int64_t)a.b.n_tokens * units) return;
-  const int row = (int)(w / units), hq0 = (int)(w - (int64_t)row * units) * rpw;
-  const int kh = hq0 / p.ratio, w2 = 2 * p.tpt, n = a.b.n_req;
+  const int w0 = blockIdx.x * 4 + (threadIdx.x >> 5), nw = gridDim.x * 4;
   const KvHead hd = *p.head;
-  int job[2] = {-1, -1};   // the prefix's and the request's own
-  if (n > 0 && row < a.b.q_start[n]) {
-    int i;
-    if (row < n && a.b.q_start[row] == row && a.b.q_start[row + 1] == row + 1) {
-      i = row;   // single tokens
-    } else {
+  const int hk = a.c.n_kv_heads, w2 = 2 * p.tpt, n = a.b.n_req;
+  for (int x = w0; x < p.ctas * 256; x += nw) {
+    const int c = x >> 8, rr = x & 255;   // CTA c's start, a row of the job there
+    if (c * hd.per >= hd.total) break;
+    const KvStart s = p.start[c];
+    if (s.off == 0) continue;
+    const KvJob job = p.jobs[s.job];
+    if (!(job.flags & JOB_ALONE) || job.nt == 0) continue;
+    const int cost = job_cost(job.nt, job.flags), w = tile_cost(job.flags);
+    const int64_t u0 = p.cost[s.job] * hk + (int64_t)s.head * cost;
+    if (u0 / hd.per != c - 1) continue;   // (cut before: the first cut's)
+    int t0, t1;   // whole in the CTA before, or here?
+    if (segment(u0, cost, w, job.nt, hd.per, c - 1, t0, t1) ? t1 == job.nt
+        : segment(u0, cost, w, job.nt, hd.per, c, t0, t1) && t0 == 0 && t1 == job.nt)
+      continue;
+    const int half = rr >> 7, r = rr & 127, tl = r / p.ratio, tok = half * p.tpt + tl;
+    if (tl >= p.tpt || tok >= job.ntok) continue;
+    Join<D> v;
+    v.add(p, hd, s.job, job, s.head, hk, 0, rr, lane);
+    v.template put<HALF>(a, (int64_t)job.tok0 + tok, s.head * p.ratio + r - tl * p.ratio, lane);
+  }
+  const int64_t all = (int64_t)a.b.n_tokens * a.n_heads, units = (int64_t)hd.prefix_jobs * w2 * a.n_heads;
+  for (int64_t x = w0; x < units; x += nw) {
+    const int slot = (int)(x / a.n_heads), hq = (int)(x - (int64_t)slot * a.n_heads);
+    const int pj = slot / w2, pt = slot - pj * w2, kh = hq / p.ratio, hl = hq - kh * p.ratio;
+    const KvJob pre = p.jobs[pj];
+    if (pt >= pre.ntok) continue;
+    const int row = pre.tok0 + pt;
+    int i = row;   // single tokens: request i has row i
+    if (!(row < n && a.b.q_start[row] == row && a.b.q_start[row + 1] == row + 1)) {
       int lo = 0, hi = n;
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -984,68 +1188,16 @@ __global__ void __launch_bounds__(128) k_kv_join(const __grid_constant__ KvAtten
     }
     const KvReq r = p.req[i];
     const int q0 = a.b.q_start[i];
-    if (r.job0 >= 0 && q0 >= 0 && row >= q0) job[1] = min(r.job0 + (row - q0) / w2, hd.jobs - 1);
-    if (r.pjob0 >= 0 && row >= r.ptok0) job[0] = min(r.pjob0 + (row - r.ptok0) / w2, hd.jobs - 1);
-  }
-  int64_t u0[2] = {0, 0};
-  int cost[2] = {0, 0}, nt[2] = {0, 0}, rr[2] = {0, 0};
-  int c0[2] = {0, 0}, c1[2] = {-1, -1};   // CTAs
-  bool done = false;
-#pragma unroll
-  for (int k = 0; k < 2; k++) {
-    if (job[k] < 0) continue;
-    const KvJob& j = p.jobs[job[k]];
-    if (j.nt <= 0 || row < j.tok0 || row - j.tok0 >= j.ntok) continue;
-    nt[k] = j.nt;
-    const int64_t at = p.cost[job[k]];
-    cost[k] = j.nt + OV;
-    u0[k] = at * a.c.n_kv_heads + (int64_t)kh * cost[k];
-    c0[k] = (int)(u0[k] / hd.per);
-    c1[k] = min((int)((u0[k] + cost[k] - 1) / hd.per), p.ctas - 1);
-    const int tok = row - j.tok0, second = j.ntok > p.tpt && tok >= p.tpt;
-    rr[k] = second * 128 + (tok - second * p.tpt) * p.ratio;   // the token's first row in the job's 256
-    int t0, t1;
-    if (k == 1 && (j.flags & JOB_ALONE)) {
-      // whole in its first CTA, or in the next when the first has only the job's own cost
-      if (segment(u0[k], cost[k], hd.per, c0[k], t0, t1)) done = t1 == j.nt;
-      else if (segment(u0[k], cost[k], hd.per, c0[k] + 1, t0, t1)) done = t0 == 0 && t1 == j.nt;
+    const int64_t home = (int64_t)row * a.n_heads + hq;
+    auto at = [&](int tok) { return (tok >= p.tpt ? 128 + (tok - p.tpt) * p.ratio : tok * p.ratio) + hl; };
+    Join<D> v;
+    v.add(p, hd, pj, pre, kh, hk, home, at(pt), lane);
+    if (r.job0 >= 0 && q0 >= 0 && row >= q0) {
+      const int j = min(r.job0 + (row - q0) / w2, hd.jobs - 1);
+      const KvJob own = p.jobs[j];
+      if (row >= own.tok0 && row - own.tok0 < own.ntok) v.add(p, hd, j, own, kh, hk, all + home, at(row - own.tok0), lane);
     }
-  }
-  if (done) return;
-  const int64_t all = (int64_t)a.b.n_tokens * a.n_heads;
-  for (int x = 0; x < rpw; x++) {
-    const int hq = hq0 + x, hl = hq - kh * p.ratio;
-    float m = -INFINITY, l = 0.0f, o[E];
-#pragma unroll
-    for (int e = 0; e < E; e++) o[e] = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 2; k++) {
-      for (int c = c0[k]; c <= c1[k]; c++) {
-        int t0, t1;
-        if (!segment(u0[k], cost[k], hd.per, c, t0, t1)) continue;
-        const bool whole = t0 == 0 && t1 == nt[k];
-        const int64_t at = whole ? (k ? all : 0) + (int64_t)row * a.n_heads + hq
-                                 : ((int64_t)c * 2 + (c == c0[k] ? 1 : 0)) * 256 + rr[k] + hl;
-        const float s = (whole ? p.home_lse : p.part_lse)[at];
-        if (s == -INFINITY) continue;
-        const float* src = (whole ? p.home : p.part) + at * D + lane * E;
-        float y[E];
-#pragma unroll
-        for (int e = 0; e < E; e++) y[e] = src[e];
-        const float m2 = fmaxf(m, s), f = m == -INFINITY ? 0.0f : ex2(__fsub_rn(m, m2)), g = ex2(__fsub_rn(s, m2));
-        l = fmaf(l, f, g);
-#pragma unroll
-        for (int e = 0; e < E; e++) o[e] = fmaf(o[e], f, __fmul_rn(g, y[e]));
-        m = m2;
-      }
-    }
-    const float inv = l == 0.0f ? 0.0f : __fdiv_rn(1.0f, l);
-    uint16_t* out = static_cast<uint16_t*>(a.out) + (int64_t)row * a.o_ts + hq * a.o_hs + lane * E;
-#pragma unroll
-    for (int e = 0; e < E; e += 2)
-      *reinterpret_cast<uint32_t*>(out + e) = pack2<HALF>(__fmul_rn(o[e], inv), __fmul_rn(o[e + 1], inv));
-    if (a.lse && lane == 0)
-      a.lse[(int64_t)row * a.n_heads + hq] = l == 0.0f ? -INFINITY : __fmul_rn(__fadd_rn(m, __log2f(l)), 0.6931471805599453f);
+    v.template put<HALF>(a, row, hq, lane);
   }
 }
 
@@ -1136,10 +1288,9 @@ cudaError_t run(const KvAttendArgs& a, const KvPlan& p, const CUtensorMap* m, cu
   if (regs * 3 < 2 * 208 + 88) return cudaErrorInvalidKernelImage;
   e = launch_after(k_kv_attend<D, HALF>, p.ctas, NT_ATT, L::SMEM, st, m[0], m[1], m[2], m[3], a, p);
   if (e != cudaSuccess) return e;
-  // a warp a row while that many warps fit on the GPU at once, else a warp a token and kv head
-  const int64_t rows = (int64_t)a.b.n_tokens * a.n_heads;
-  const int rpw = rows <= (int64_t)p.ctas * 64 ? 1 : p.ratio;
-  return launch_after(k_kv_join<D, HALF>, (unsigned)((rows / rpw + 3) / 4), 128, 0, st, a, p, rpw);
+  // a warp a row; no more than the GPU holds at once
+  const int64_t rows = std::max<int64_t>((int64_t)p.ctas * 256, a.b.n_groups ? (int64_t)a.b.n_tokens * a.n_heads : 0);
+  return launch_after(k_kv_join<D, HALF>, (unsigned)std::min<int64_t>((rows + 3) / 4, (int64_t)p.ctas * 8), 128, 0, st, a, p);
 }
 
 }  // namespace
