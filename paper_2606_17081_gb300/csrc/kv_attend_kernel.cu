@@ -20,6 +20,7 @@
 
 #include <algorithm>
 #include <climits>
+#include <cstring>
 
 #include "rs_internal.h"
 
@@ -51,6 +52,17 @@ struct __align__(16) KvJob {
   int32_t nt;           // tiles of them
   int32_t lim0;         // keys that the first token sees; the next see one more each
   int32_t flags;
+  int64_t cost;         // of the jobs before, for one kv head
+  int64_t reserved0;
+};
+
+// A job and head that a share's end cuts, at the share's end that cuts it first.
+struct __align__(16) KvCut {
+  int32_t tok0, ntok;   // (ntok 0: none)
+  int32_t head;
+  int32_t c0;           // the CTA in which it begins
+  int32_t first, last;  // CTAs that have tiles of it
+  int32_t reserved0, reserved1;
 };
 
 struct KvHead {
@@ -62,19 +74,14 @@ struct KvStart {
   int32_t job, head, off, reserved0;   // where a CTA's share begins
 };
 
-// Jobs of a request's rows.
-struct KvReq {
-  int32_t job0;    // its first own job
-};
-
 struct KvPlan {
   KvHead* head;
   KvJob* jobs;          // [cap + 1]
-  int64_t* cost;        // [cap + 1] cost of the jobs before, for one kv head
-  KvReq* req;           // [n_req]
-  int32_t* gjob;        // [n_groups] first prefix job, -1: not shared
+  int32_t* job0;        // [n_req] first own job, or -1
+  int32_t* gjob;        // [n_groups] first prefix job, -1: not shared (more than PLAN_GROUPS groups)
   unsigned long long* gsum;   // [4 n_groups] (more than PLAN_GROUPS groups)
   KvStart* start;       // [ctas]
+  KvCut* cut;           // [ctas]
   float* part;          // [ctas][2][256][D] cut jobs' rows: of the first cut job (0), of the last (1)
   float* part_lse;      // [ctas][2][256]
   float* home;          // [2][rows][D] rows with a prefix job and an own one, each whole
@@ -119,29 +126,8 @@ __device__ int64_t block_scan(int64_t x, int64_t* sm, int64_t* total) {
 
 struct ReqLens {
   int q0, q, kv;   // first row, rows, context with them
+  int g;           // group, or -1
 };
-
-__device__ __forceinline__ ReqLens kv_req(const rs_kv_batch& b, int i) {
-  ReqLens r;
-  r.q0 = clampi(b.q_start[i], 0, b.n_tokens);
-  r.q = max(clampi(b.q_start[i + 1], 0, b.n_tokens) - r.q0, 0);
-  r.kv = clampi(b.kv_len[i], 0, INT_MAX - 1);
-  return r;
-}
-
-__device__ __forceinline__ int group_of(const rs_kv_batch& b, int i) {
-  if (b.n_groups == 0 || i < b.group_start[0] || i >= b.group_start[b.n_groups]) return -1;
-  int lo = 0, hi = b.n_groups;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (b.group_start[mid] <= i) lo = mid; else hi = mid;
-  }
-  return lo;
-}
-
-__device__ __forceinline__ int prefix_keys(const rs_kv_batch& b, int g) {
-  return (int)min((int64_t)(max(b.prefix_len[g], 0) & ~15), (int64_t)b.max_blocks * 16);
-}
 
 __device__ __forceinline__ int tiles(int keys) { return keys > 0 ? (keys + TK - 1) / TK : 0; }
 
@@ -153,40 +139,97 @@ __device__ __forceinline__ int job_cost(int nt, int flags) {
 // The first tile that starts at cost `off` of a job or after it.
 __device__ __forceinline__ int tile_at(int off, int w) { return off <= OV ? 0 : (off - OV + w - 1) / w; }
 
+// The tiles that CTA c has of a job and head of `cost` from u0 on.
+__device__ __forceinline__ bool segment(int64_t u0, int cost, int w, int nt, int64_t per, int64_t c, int& t0, int& t1) {
+  const int64_t lo = max(c * per, u0) - u0, hi = min((c + 1) * per, u0 + cost) - u0;
+  if (lo >= hi) return false;
+  t0 = min(tile_at((int)lo, w), nt);
+  t1 = min(tile_at((int)hi, w), nt);
+  return t1 > t0;
+}
+
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
 // One CTA: whether each group's prefix pays as one job for all its rows, the
-// jobs, their costs' sums, and every CTA's start.  Latency is all that counts
-// here (a few dependent reads and block sums); sums live in shared memory at
+// jobs, their costs' sums, every CTA's start and what its end cuts.  Latency is
+// all that counts here (a few dependent reads and block sums): lengths are read
+// once at up to NT_PLAN requests, sums and costs live in shared memory at
 // ordinary sizes.
 __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, int n_kv_heads) {
   extern __shared__ unsigned long long psm[];
   int64_t* s_cost = reinterpret_cast<int64_t*>(psm);            // [PLAN_JOBS + 1]
   unsigned long long* s_sum = psm + PLAN_JOBS + 1;               // [4 PLAN_GROUPS]
+  int32_t* s_start = reinterpret_cast<int32_t*>(s_sum + 4 * PLAN_GROUPS);   // [PLAN_GROUPS + 1]
+  int32_t* s_prefix = s_start + PLAN_GROUPS + 1;                 // [PLAN_GROUPS]
+  int32_t* s_gjob = s_prefix + PLAN_GROUPS;                      // [PLAN_GROUPS]
   __shared__ int64_t s_scan[NT_PLAN / 32];
   const int tid = threadIdx.x, n = b.n_req, G = b.n_groups;
   const int w2 = 2 * p.tpt;
-  unsigned long long* sum = G <= PLAN_GROUPS ? s_sum : p.gsum;
+  const bool few = G <= PLAN_GROUPS;
+  unsigned long long* sum = few ? s_sum : p.gsum;
+  const int32_t* gstart = few ? s_start : b.group_start;
+  const int32_t* glen = few ? s_prefix : b.prefix_len;
+  int32_t* gjob = few ? s_gjob : p.gjob;
   asm volatile("griddepcontrol.launch_dependents;");
 
+  auto of = [&](int x) { return few ? s_sum[x] : __ldcg(p.gsum + x); };
+  auto prefix_keys = [&](int g) { return (int)min((int64_t)(max(glen[g], 0) & ~15), (int64_t)b.max_blocks * 16); };
+  auto rows_at = [&](int i) { return clampi(b.q_start[i], 0, b.n_tokens); };
+  auto lens = [&](int i) {
+    ReqLens r;
+    r.q0 = rows_at(i);
+    r.q = max(rows_at(i + 1) - r.q0, 0);
+    r.kv = clampi(b.kv_len[i], 0, INT_MAX - 1);
+    return r;
+  };
+  auto group = [&](int i) {
+    if (G == 0 || i < gstart[0] || i >= gstart[G]) return -1;
+    int lo = 0, hi = G;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (gstart[mid] <= i) lo = mid; else hi = mid;
+    }
+    return lo;
+  };
+  ReqLens mine{0, 0, 0, -1};   // of request tid
+  if (tid < n) mine = lens(tid);
+  const int q_end = n > 0 ? rows_at(n) : 0;
+  if (few && G > 0) {
+    for (int g = tid; g <= G; g += NT_PLAN) s_start[g] = b.group_start[g];
+    for (int g = tid; g < G; g += NT_PLAN) s_prefix[g] = b.prefix_len[g];
+  }
   // of each group: its requests' costs without and with a shared prefix, whether
   // some row sees less than the prefix, the longest context
-  auto of = [&](int x) { return G <= PLAN_GROUPS ? s_sum[x] : __ldcg(p.gsum + x); };
   for (int x = tid; x < 4 * G; x += NT_PLAN) sum[x] = 0;
   __syncthreads();
+  mine.g = tid < n ? group(tid) : -1;
+  auto request = [&](int i) {
+    if (i == tid) return mine;
+    ReqLens r = lens(i);
+    r.g = group(i);
+    return r;
+  };
   if (G > 0) {
     for (int i = tid; i < n; i += NT_PLAN) {
-      const int g = group_of(b, i);
-      const ReqLens r = kv_req(b, i);
+      const ReqLens r = request(i);
+      const int g = r.g;
       if (g < 0 || r.q == 0) continue;
-      const int P = prefix_keys(b, g), rt = (r.q + w2 - 1) / w2, seen = r.kv - (r.q >> 1);
-      const int t = tiles(seen), ts = tiles(seen - P);
+      const int P = prefix_keys(g), rt = (r.q + w2 - 1) / w2, seen = r.kv - (r.q >> 1);
       const int fl = r.q > p.tpt ? JOB_WIDE : 0;
-      atomicAdd(&sum[4 * g], (unsigned long long)rt * job_cost(t, fl));
-      atomicAdd(&sum[4 * g + 1], (unsigned long long)rt * job_cost(ts, fl));
+      atomicAdd(&sum[4 * g], (unsigned long long)rt * job_cost(tiles(seen), fl));
+      atomicAdd(&sum[4 * g + 1], (unsigned long long)rt * job_cost(tiles(seen - P), fl));
       if (r.kv - r.q + 1 < P) sum[4 * g + 2] = 1;
       atomicMax(&sum[4 * g + 3], (unsigned long long)r.kv);
     }
     __syncthreads();
   }
+  auto put = [&](int64_t at, const KvJob& j) {
+    if (at >= p.cap) return;
+    p.jobs[at] = j;
+    if (at < PLAN_JOBS) s_cost[at] = job_cost(j.nt, j.flags);
+  };
   // prefix jobs.  Shared when that costs less: the group's prefix once for every
   // w2 of its tokens, and a quarter of a tile a token for the parts' way
   // through memory (2 parts written and read, 4 D bytes each a row, against
@@ -196,13 +239,12 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
     const int g = base + tid;
     int cnt = 0, t0 = 0, t1 = 0, P = 0, first = 0;
     if (g < G) {
-      first = clampi(b.group_start[g], 0, n);
-      const int last = clampi(b.group_start[g + 1], 0, n);
-      P = prefix_keys(b, g);
-      t0 = clampi(b.q_start[first], 0, b.n_tokens);
-      t1 = clampi(b.q_start[max(first, last)], 0, b.n_tokens);
+      first = clampi(gstart[g], 0, n);
+      const int last = clampi(gstart[g + 1], 0, n);
+      t0 = rows_at(first);
+      t1 = rows_at(max(first, last));
       const int rt = t1 > t0 ? (t1 - t0 + w2 - 1) / w2 : 0;
-      P = (int)min((unsigned long long)P, of(4 * g + 3));   // (a prefix that nobody has written yet is not read)
+      P = (int)min((unsigned long long)prefix_keys(g), of(4 * g + 3));   // (what nobody has written yet is not read)
       const unsigned long long with = of(4 * g + 1) + (unsigned long long)rt * job_cost(tiles(P), t1 - t0 > p.tpt ? JOB_WIDE : 0) +
                                       (unsigned long long)(max(t1 - t0, 0) >> 1);
       if (P > 0 && first < last && with < of(4 * g)) cnt = rt;
@@ -211,23 +253,19 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
     jobs += total;
     if (g < G) {
       const bool fits = cnt > 0 && at + cnt <= p.cap;
-      p.gjob[g] = fits ? (int32_t)at : -1;
+      gjob[g] = fits ? (int32_t)at : -1;
       const bool even = of(4 * g + 2) == 0;
-      for (int k = 0; k < cnt && at + k < p.cap; k++) {
+      for (int k = 0; k < cnt; k++) {
         KvJob j = {};
-        if (!fits) {   // (starts that decrease: no work)
-          p.jobs[at + k] = j;
-          continue;
+        if (fits) {   // (else starts decrease: no work)
+          j.tok0 = t0 + k * w2;
+          j.ntok = min(w2, t1 - j.tok0);
+          j.row = first;
+          j.kend = j.lim0 = P;
+          j.nt = tiles(P);
+          j.flags = JOB_PREFIX | (even ? JOB_EVEN : 0) | (j.ntok > p.tpt ? JOB_WIDE : 0);
         }
-        j.tok0 = t0 + k * w2;
-        j.ntok = min(w2, t1 - j.tok0);
-        j.row = first;
-        j.key0 = 0;
-        j.kend = P;
-        j.nt = tiles(P);
-        j.lim0 = P;
-        j.flags = JOB_PREFIX | (even ? JOB_EVEN : 0) | (j.ntok > p.tpt ? JOB_WIDE : 0);
-        p.jobs[at + k] = j;
+        put(at + k, j);
       }
     }
   }
@@ -237,27 +275,22 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
   // the requests' own jobs
   for (int base = 0; base < n; base += NT_PLAN) {
     const int i = base + tid;
-    ReqLens r{0, 0, 0};
-    int key0 = 0, cnt = 0, pj = -1;
+    ReqLens r{0, 0, 0, -1};
+    int key0 = 0, cnt = 0;
+    bool alone = true;
     if (i < n) {
-      r = kv_req(b, i);
-      const int g = group_of(b, i);
-      if (g >= 0 && p.gjob[g] >= 0) {
-        pj = p.gjob[g];
-        key0 = prefix_keys(b, g);
+      r = request(i);
+      if (r.g >= 0 && gjob[r.g] >= 0) {
+        alone = false;
+        key0 = prefix_keys(r.g);
       }
       cnt = (r.q + w2 - 1) / w2;
     }
     const int64_t at = jobs + block_scan(cnt, s_scan, &total);
     jobs += total;
-    const bool fits = cnt > 0 && at + cnt <= p.cap;
-    if (i < n) p.req[i] = KvReq{fits ? (int32_t)at : -1};
-    // a request of one job is its thread's; a longer one is its warp's
-    for (int k = 0; !fits && k < cnt && at + k < p.cap; k++) p.jobs[at + k] = KvJob{};   // (as above)
-    unsigned todo = __ballot_sync(~0u, fits);
-    const unsigned mine = 1u << (tid & 31);
-    const unsigned lone = __ballot_sync(~0u, fits && cnt == 1);
-    auto put = [&](int64_t at, int k, int i, int q0, int q, int kv, int key0, int pj) {
+    const bool fits = at + cnt <= p.cap;
+    if (i < n) p.job0[i] = cnt > 0 && fits ? (int32_t)at : -1;
+    auto job = [&](int k, int i, int q0, int q, int kv, int key0, bool alone) {
       KvJob j;
       const int a = k * w2, e = min(a + w2, q);
       j.tok0 = q0 + a;
@@ -267,44 +300,42 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
       j.kend = clampi((int64_t)kv - q + e, 0, (int)min((int64_t)b.max_blocks * 16, (int64_t)INT_MAX - 256));
       j.nt = tiles(j.kend - key0);
       j.lim0 = kv - q + a + 1;
-      j.flags = (pj < 0 ? JOB_ALONE : 0) | (j.ntok > p.tpt ? JOB_WIDE : 0);
-      p.jobs[at + k] = j;
+      j.flags = (alone ? JOB_ALONE : 0) | (j.ntok > p.tpt ? JOB_WIDE : 0);
+      return j;
     };
-    if (lone & mine) put(at, 0, i, r.q0, r.q, r.kv, key0, pj);
-    todo &= ~lone;
-    while (todo) {
+    // a request of one job is its thread's; a longer one is its warp's
+    if (cnt == 1) put(at, fits ? job(0, i, r.q0, r.q, r.kv, key0, alone) : KvJob{});
+    for (unsigned todo = __ballot_sync(~0u, cnt > 1); todo; todo &= todo - 1) {
       const int src = __ffs(todo) - 1;
-      todo &= todo - 1;
       const int64_t sat = __shfl_sync(~0u, at, src);
       const int sc = __shfl_sync(~0u, cnt, src), si = __shfl_sync(~0u, i, src);
       const int s0 = __shfl_sync(~0u, r.q0, src), sq = __shfl_sync(~0u, r.q, src);
       const int sk = __shfl_sync(~0u, r.kv, src), s1 = __shfl_sync(~0u, key0, src);
-      const int sp = __shfl_sync(~0u, pj, src);
-      for (int k = tid & 31; k < sc; k += 32) put(sat, k, si, s0, sq, sk, s1, sp);
+      const bool sa = __shfl_sync(~0u, (int)alone, src), sf = __shfl_sync(~0u, (int)fits, src);
+      for (int k = tid & 31; k < sc; k += 32) put(sat + k, sf ? job(k, si, s0, sq, sk, s1, sa) : KvJob{});
     }
   }
   // rows of no request: jobs without keys
-  const int q_end = n > 0 ? clampi(b.q_start[n], 0, b.n_tokens) : 0;
   const int pads = (b.n_tokens - q_end + w2 - 1) / w2;
-  for (int k = tid; k < pads && jobs + k < p.cap; k += NT_PLAN) {
+  for (int k = tid; k < pads; k += NT_PLAN) {
     KvJob j = {};
     j.tok0 = q_end + k * w2;
     j.ntok = min(w2, b.n_tokens - j.tok0);
     j.flags = JOB_ALONE | (j.ntok > p.tpt ? JOB_WIDE : 0);
-    p.jobs[jobs + k] = j;
+    put(jobs + k, j);
   }
   const int J = (int)min(jobs + pads, (int64_t)p.cap);
   __syncthreads();   // the jobs
   int64_t cost = 0;
-  for (int base = 0; base <= J; base += NT_PLAN) {
+  for (int base = 0; base < J; base += NT_PLAN) {
     const int j = base + tid;
     int64_t c = 0;
-    if (j < J) c = job_cost(p.jobs[j].nt, p.jobs[j].flags);
+    if (j < J) c = j < PLAN_JOBS ? s_cost[j] : job_cost(p.jobs[j].nt, p.jobs[j].flags);
     const int64_t at = cost + block_scan(c, s_scan, &total);
     cost += total;
-    if (j <= J) {
-      p.cost[j] = at;
-      if (j <= PLAN_JOBS) s_cost[j] = at;
+    if (j < J) {
+      p.jobs[j].cost = at;
+      if (j < PLAN_JOBS) s_cost[j] = at;
     }
   }
   __syncthreads();
@@ -312,22 +343,37 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
   // two tiles at least, one for each stream of a CTA
   const int64_t per = max((all + p.ctas - 1) / p.ctas, (int64_t)(2 * W_NARROW + OV));
   if (tid == 0) *p.head = KvHead{all, per, J, prefix_jobs};
-  const int64_t* cs = J <= PLAN_JOBS ? s_cost : p.cost;
   for (int c = tid; c < p.ctas; c += NT_PLAN) {
     const int64_t u = c * per;
     KvStart s{0, 0, 0, 0};
+    KvCut cut = {};
     if (u < all) {
       int lo = 0, hi = J;   // the last job that starts at or before u
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (cs[mid] * n_kv_heads <= u) lo = mid; else hi = mid;
+        const int64_t at = mid < PLAN_JOBS ? s_cost[mid] : p.jobs[mid].cost;
+        if (at * n_kv_heads <= u) lo = mid; else hi = mid;
       }
-      const int64_t cj = cs[lo + 1] - cs[lo], in = u - cs[lo] * n_kv_heads;
+      const KvJob j = p.jobs[lo];
+      const int cj = job_cost(j.nt, j.flags);
+      const int64_t in = u - j.cost * n_kv_heads;
       s.job = lo;
-      s.head = (int)(in / cj);
-      s.off = (int)(in - s.head * cj);
+      s.head = (int)quotient(in, cj);
+      s.off = (int)(in - (int64_t)s.head * cj);
+      const int64_t u0 = u - s.off;
+      if (s.off > 0 && j.nt > 0 && (j.flags & JOB_ALONE) && u0 >= u - per) {   // not cut before
+        const int w = tile_cost(j.flags);
+        int t0, t1, e = (int)quotient(u0 + cj - 1, per);
+        cut.c0 = c - 1;
+        cut.first = segment(u0, cj, w, j.nt, per, c - 1, t0, t1) ? c - 1 : c;
+        cut.last = segment(u0, cj, w, j.nt, per, e, t0, t1) ? e : e - 1;
+        cut.tok0 = j.tok0;
+        cut.head = s.head;
+        cut.ntok = cut.first < cut.last ? j.ntok : 0;   // (else whole in one CTA)
+      }
     }
     p.start[c] = s;
+    p.cut[c] = cut;
   }
 }
 
@@ -692,8 +738,8 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
   __syncthreads();
   tc_after();
   const uint32_t tmem = *s_tmem;
-  asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");   // the plan
+  asm volatile("griddepcontrol.launch_dependents;");
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
@@ -1084,121 +1130,172 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
 
 // ------------------------------------------------------------------ joining
 
-// The tiles that CTA c has of a job and head of `cost` from u0 on.
-__device__ __forceinline__ bool segment(int64_t u0, int cost, int w, int nt, int64_t per, int64_t c, int& t0, int& t1) {
-  const int64_t lo = max(c * per, u0) - u0, hi = min((c + 1) * per, u0 + cost) - u0;
-  if (lo >= hi) return false;
-  t0 = min(tile_at((int)lo, w), nt);
-  t1 = min(tile_at((int)hi, w), nt);
-  return t1 > t0;
-}
-
-// Parts of one row (token, head).
-template <int D>
-struct Join {
-  static constexpr int E = D / 32;
-  float m, l, o[E];
-  __device__ Join() : m(-INFINITY), l(0.0f) {
-#pragma unroll
-    for (int e = 0; e < E; e++) o[e] = 0.0f;
-  }
-  // those of row rr of 256 of job j, head kh
-  __device__ void add(const KvPlan& p, const KvHead& hd, int j, const KvJob& job, int kh, int n_kv_heads,
-                      int64_t home, int rr, int lane) {
-    if (job.nt <= 0) return;
-    const int w = tile_cost(job.flags), cost = job_cost(job.nt, job.flags);
-    const int64_t u0 = p.cost[j] * n_kv_heads + (int64_t)kh * cost;
-    const int c0 = (int)(u0 / hd.per), c1 = min((int)((u0 + cost - 1) / hd.per), p.ctas - 1);
-    for (int c = c0; c <= c1; c++) {
-      int t0, t1;
-      if (!segment(u0, cost, w, job.nt, hd.per, c, t0, t1)) continue;
-      const bool whole = t0 == 0 && t1 == job.nt;
-      const int64_t at = whole ? home : ((int64_t)c * 2 + (c == c0 ? 1 : 0)) * 256 + rr;
-      const float s = (whole ? p.home_lse : p.part_lse)[at];
-      const float* src = (whole ? p.home : p.part) + at * D + lane * E;
-      float y[E];
-#pragma unroll
-      for (int e = 0; e < E; e++) y[e] = src[e];
-      if (s == -INFINITY) continue;
-      const float m2 = fmaxf(m, s), f = m == -INFINITY ? 0.0f : ex2(__fsub_rn(m, m2)), g = ex2(__fsub_rn(s, m2));
-      l = fmaf(l, f, g);
-#pragma unroll
-      for (int e = 0; e < E; e++) o[e] = fmaf(o[e], f, __fmul_rn(g, y[e]));
-      m = m2;
-    }
-  }
-  template <bool HALF>
-  __device__ void put(const KvAttendArgs& a, int64_t row, int hq, int lane) const {
-    const float inv = l == 0.0f ? 0.0f : __fdiv_rn(1.0f, l);
-    uint16_t* out = static_cast<uint16_t*>(a.out) + row * a.o_ts + hq * a.o_hs + lane * E;
-#pragma unroll
-    for (int e = 0; e < E; e += 2)
-      *reinterpret_cast<uint32_t*>(out + e) = pack2<HALF>(__fmul_rn(o[e], inv), __fmul_rn(o[e + 1], inv));
-    if (a.lse && lane == 0)
-      a.lse[row * a.n_heads + hq] = l == 0.0f ? -INFINITY : __fmul_rn(__fadd_rn(m, __log2f(l)), 0.6931471805599453f);
-  }
+// Where the parts of a job and head are: whole in its place among all rows (one
+// part, last < first), or in CTAs first .. last.
+struct Parts {
+  int c0, first, last, count;
 };
 
-// Rows that have parts, a warp a row: those of the jobs that a share's end cut
-// (first looked for at each CTA's start), and those of shared groups, which
-// have a prefix job and an own one.  The order of the parts is the keys'.
+__device__ __forceinline__ Parts parts_of(const KvJob& j, int head, int n_kv_heads, const KvHead& hd) {
+  Parts r{0, 0, 0, 0};
+  if (j.nt <= 0) return r;
+  const int w = tile_cost(j.flags), cost = job_cost(j.nt, j.flags);
+  const int64_t u0 = j.cost * n_kv_heads + (int64_t)head * cost;
+  const int64_t c0 = quotient(u0, hd.per), c1 = quotient(u0 + cost - 1, hd.per);
+  int t0, t1;
+  r.c0 = (int)c0;
+  r.first = (int)(segment(u0, cost, w, j.nt, hd.per, c0, t0, t1) ? c0 : c0 + 1);
+  r.last = (int)(segment(u0, cost, w, j.nt, hd.per, c1, t0, t1) ? c1 : c1 - 1);
+  r.count = max(r.last - r.first + 1, 1);
+  if (r.count == 1) r.last = r.first - 1;
+  return r;
+}
+
+__device__ __forceinline__ KvJob job_from_l2(const KvJob* j) {
+  KvJob r;
+  const int4* s = reinterpret_cast<const int4*>(j);
+  int4* d = reinterpret_cast<int4*>(&r);
+#pragma unroll
+  for (int k = 0; k < 3; k++) d[k] = __ldcg(s + k);
+  return r;
+}
+
+// One row (token, head) from its parts: x's (row rx of the 256 if cut, else at
+// home), then y's.  A lane takes the log sum of a part, the warp their largest
+// and the weights, and the rows of several parts are on their way at once.
 template <int D, bool HALF>
-__global__ void __launch_bounds__(128) k_kv_join(const __grid_constant__ KvAttendArgs a,
-                                                 const __grid_constant__ KvPlan p) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int lane = threadIdx.x & 31;
-  const int w0 = blockIdx.x * 4 + (threadIdx.x >> 5), nw = gridDim.x * 4;
-  const KvHead hd = *p.head;
-  const int hk = a.c.n_kv_heads, w2 = 2 * p.tpt, n = a.b.n_req;
-  for (int x = w0; x < p.ctas * 256; x += nw) {
-    const int c = x >> 8, rr = x & 255;   // CTA c's start, a row of the job there
-    if (c * hd.per >= hd.total) break;
-    const KvStart s = p.start[c];
-    if (s.off == 0) continue;
-    const KvJob job = p.jobs[s.job];
-    if (!(job.flags & JOB_ALONE) || job.nt == 0) continue;
-    const int cost = job_cost(job.nt, job.flags), w = tile_cost(job.flags);
-    const int64_t u0 = p.cost[s.job] * hk + (int64_t)s.head * cost;
-    if (u0 / hd.per != c - 1) continue;   // (cut before: the first cut's)
-    int t0, t1;   // whole in the CTA before, or here?
-    if (segment(u0, cost, w, job.nt, hd.per, c - 1, t0, t1) ? t1 == job.nt
-        : segment(u0, cost, w, job.nt, hd.per, c, t0, t1) && t0 == 0 && t1 == job.nt)
-      continue;
-    const int half = rr >> 7, r = rr & 127, tl = r / p.ratio, tok = half * p.tpt + tl;
-    if (tl >= p.tpt || tok >= job.ntok) continue;
-    Join<D> v;
-    v.add(p, hd, s.job, job, s.head, hk, 0, rr, lane);
-    v.template put<HALF>(a, (int64_t)job.tok0 + tok, s.head * p.ratio + r - tl * p.ratio, lane);
-  }
-  const int64_t all = (int64_t)a.b.n_tokens * a.n_heads, units = (int64_t)hd.prefix_jobs * w2 * a.n_heads;
-  for (int64_t x = w0; x < units; x += nw) {
-    const int slot = (int)(x / a.n_heads), hq = (int)(x - (int64_t)slot * a.n_heads);
-    const int pj = slot / w2, pt = slot - pj * w2, kh = hq / p.ratio, hl = hq - kh * p.ratio;
-    const KvJob pre = p.jobs[pj];
-    if (pt >= pre.ntok) continue;
-    const int row = pre.tok0 + pt;
-    int i = row;   // single tokens: request i has row i
-    if (!(row < n && a.b.q_start[row] == row && a.b.q_start[row + 1] == row + 1)) {
-      int lo = 0, hi = n;
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.b.q_start[mid] <= row) lo = mid; else hi = mid;
+__device__ __forceinline__ void join_row(const KvAttendArgs& a, const KvPlan& p, const Parts& x, int rx, const Parts& y, int ry,
+                                         int64_t row, int hq, int lane) {
+  constexpr int E = D / 32;
+  const int64_t home = row * a.n_heads + hq, all = (int64_t)a.b.n_tokens * a.n_heads;
+  const int count = x.count + y.count;
+  float m = -INFINITY, l = 0.0f, o[E];
+#pragma unroll
+  for (int e = 0; e < E; e++) o[e] = 0.0f;
+  for (int base = 0; base < count; base += 32) {
+    const int k = base + lane;
+    const float* src = nullptr;
+    float s = -INFINITY;
+    if (k < count) {
+      const Parts& q = k < x.count ? x : y;
+      const int c = q.first + (k < x.count ? k : k - x.count);
+      const bool whole = q.last < q.first;
+      const int64_t at = whole ? (k < x.count ? 0 : all) + home
+                               : ((int64_t)c * 2 + (c == q.c0 ? 1 : 0)) * 256 + (k < x.count ? rx : ry);
+      s = (whole ? p.home_lse : p.part_lse)[at];
+      src = (whole ? p.home : p.part) + at * D;
+    }
+    float big = s;
+#pragma unroll
+    for (int z = 16; z; z >>= 1) big = fmaxf(big, __shfl_xor_sync(~0u, big, z));
+    const float m2 = fmaxf(m, big);
+    const float wt = s == -INFINITY ? 0.0f : ex2(__fsub_rn(s, m2));
+    const float f = m == -INFINITY ? 0.0f : ex2(__fsub_rn(m, m2));
+    float sum = wt;
+#pragma unroll
+    for (int z = 16; z; z >>= 1) sum = __fadd_rn(sum, __shfl_xor_sync(~0u, sum, z));
+    l = fmaf(l, f, sum);
+#pragma unroll
+    for (int e = 0; e < E; e++) o[e] = __fmul_rn(o[e], f);
+    m = m2;
+    const int here = min(32, count - base);
+    for (int q = 0; q < here; q += 4) {
+      float w4[4], v[4][E];
+#pragma unroll
+      for (int z = 0; z < 4; z++) {   // (lanes past the last part have weight 0 and the first one's row)
+        const int from = min(q + z, here - 1);
+        w4[z] = q + z < here ? __shfl_sync(~0u, wt, from) : 0.0f;
+        const float* r = reinterpret_cast<const float*>(__shfl_sync(~0u, reinterpret_cast<unsigned long long>(src), from)) + lane * E;
+        if constexpr (E == 4) {
+          const float4 t = *reinterpret_cast<const float4*>(r);
+          v[z][0] = t.x; v[z][1] = t.y; v[z][2] = t.z; v[z][3] = t.w;
+        } else {
+          const float2 t = *reinterpret_cast<const float2*>(r);
+          v[z][0] = t.x; v[z][1] = t.y;
+        }
       }
-      i = lo;
+#pragma unroll
+      for (int z = 0; z < 4; z++)
+#pragma unroll
+        for (int e = 0; e < E; e++) o[e] = w4[z] == 0.0f ? o[e] : fmaf(w4[z], v[z][e], o[e]);
     }
-    const KvReq r = p.req[i];
-    const int q0 = a.b.q_start[i];
-    const int64_t home = (int64_t)row * a.n_heads + hq;
-    auto at = [&](int tok) { return (tok >= p.tpt ? 128 + (tok - p.tpt) * p.ratio : tok * p.ratio) + hl; };
-    Join<D> v;
-    v.add(p, hd, pj, pre, kh, hk, home, at(pt), lane);
-    if (r.job0 >= 0 && q0 >= 0 && row >= q0) {
-      const int j = min(r.job0 + (row - q0) / w2, hd.jobs - 1);
-      const KvJob own = p.jobs[j];
-      if (row >= own.tok0 && row - own.tok0 < own.ntok) v.add(p, hd, j, own, kh, hk, all + home, at(row - own.tok0), lane);
-    }
-    v.template put<HALF>(a, row, hq, lane);
   }
+  const float inv = l == 0.0f ? 0.0f : __fdiv_rn(1.0f, l);
+  uint16_t* out = static_cast<uint16_t*>(a.out) + row * a.o_ts + hq * a.o_hs + lane * E;
+  uint32_t z[E / 2];
+#pragma unroll
+  for (int e = 0; e < E; e += 2) z[e / 2] = pack2<HALF>(__fmul_rn(o[e], inv), __fmul_rn(o[e + 1], inv));
+  if constexpr (E == 4) *reinterpret_cast<uint2*>(out) = make_uint2(z[0], z[1]);
+  else *reinterpret_cast<uint32_t*>(out) = z[0];
+  if (a.lse && lane == 0)
+    a.lse[home] = l == 0.0f ? -INFINITY : __fmul_rn(__fadd_rn(m, __log2f(l)), 0.6931471805599453f);
+}
+
+// Rows that have parts, a warp a row: of the jobs that a share's end cut (a CTA
+// for 32 of the job's 256), and of shared groups, whose rows have a prefix job
+// and an own one (a CTA for 8).  The parts' order is the keys', so the result
+// does not depend on when they came.  What the plan says is read before the
+// attention kernel has ended (the plan had, when it let this one start).
+template <int D, bool HALF>
+__global__ void __launch_bounds__(256) k_kv_join(const __grid_constant__ KvAttendArgs a,
+                                                 const __grid_constant__ KvPlan p) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int hk = a.c.n_kv_heads, w2 = 2 * p.tpt, n = a.b.n_req;
+  bool waited = false;
+  auto wait = [&]() {
+    if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
+    waited = true;
+  };
+  const int cuts = p.ctas * 8;
+  int64_t task = blockIdx.x;
+  for (; task < cuts; task += gridDim.x) {
+    const int4* c = reinterpret_cast<const int4*>(p.cut + (task >> 3));
+    const int4 c0 = __ldcg(c), c1 = __ldcg(c + 1);
+    const int r0 = (int)(task & 7) * 32 + warp * 4, half = r0 >> 7;   // the warp's four rows
+    const Parts x{c0.w, c1.x, c1.y, c1.y - c1.x + 1}, none{0, 0, 0, 0};
+    for (int k = 0; k < 4; k++) {
+      const int r = (r0 & 127) + k, tl = r / p.ratio, tok = half * p.tpt + tl;
+      if (tl >= p.tpt || tok >= c0.y) break;
+      wait();
+      join_row<D, HALF>(a, p, x, r0 + k, none, 0, (int64_t)c0.x + tok, c0.z * p.ratio + r - tl * p.ratio, lane);
+    }
+  }
+  if (a.b.n_groups > 0) {
+    KvHead hd;
+    const int4 h0 = __ldcg(reinterpret_cast<const int4*>(p.head)), h1 = __ldcg(reinterpret_cast<const int4*>(p.head) + 1);
+    memcpy(&hd, &h0, 16);
+    memcpy(reinterpret_cast<char*>(&hd) + 16, &h1, 8);
+    for (task -= cuts; task < (int64_t)hd.prefix_jobs * hk * 32; task += gridDim.x) {
+      const int pj = (int)((task >> 5) / hk), kh = (int)((task >> 5) - (int64_t)pj * hk);
+      const KvJob pre = job_from_l2(p.jobs + pj);
+      const int rr = (int)(task & 31) * 8 + warp, r = rr & 127, tl = r / p.ratio, hl = r - tl * p.ratio;
+      const int tok = (rr >> 7) * p.tpt + tl;
+      if (tl >= p.tpt || tok >= pre.ntok) continue;
+      const int row = pre.tok0 + tok;
+      int i = row;   // single tokens: request i has row i
+      if (!(row < n && __ldcg(a.b.q_start + row) == row && __ldcg(a.b.q_start + row + 1) == row + 1)) {
+        int lo = 0, hi = n;
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (__ldcg(a.b.q_start + mid) <= row) lo = mid; else hi = mid;
+        }
+        i = lo;
+      }
+      const int j0 = __ldcg(p.job0 + i), q0 = __ldcg(a.b.q_start + i);
+      Parts own{0, 0, 0, 0};
+      int ro = 0;
+      if (j0 >= 0 && q0 >= 0 && row >= q0) {
+        const KvJob j = job_from_l2(p.jobs + min(j0 + (row - q0) / w2, hd.jobs - 1));
+        const int t = row - j.tok0;
+        if (t >= 0 && t < j.ntok) own = parts_of(j, kh, hk, hd);
+        ro = (t >= p.tpt ? 128 + (t - p.tpt) * p.ratio : t * p.ratio) + hl;
+      }
+      const Parts x = parts_of(pre, kh, hk, hd);
+      wait();
+      join_row<D, HALF>(a, p, x, rr, own, ro, row, kh * p.ratio + hl, lane);
+    }
+  }
+  wait();   // (no CTA ends before the attention kernel: the next call's plan waits for this one)
 }
 
 // ------------------------------------------------------------------ host
@@ -1262,11 +1359,11 @@ size_t carve(const KvAttendArgs& a, int ctas, unsigned char* ws, KvPlan& p) {
   };
   take(p.head, 1);
   take(p.jobs, (size_t)p.cap + 1);
-  take(p.cost, (size_t)p.cap + 1);
-  take(p.req, n);
-  take(p.gjob, G);
+  take(p.job0, n);
+  take(p.gjob, G > PLAN_GROUPS ? G : 0);
   take(p.gsum, G > PLAN_GROUPS ? 4 * G : 0);
   take(p.start, ctas);
+  take(p.cut, ctas);
   take(p.part, (size_t)ctas * 2 * 256 * D);
   take(p.part_lse, (size_t)ctas * 2 * 256);
   take(p.home, G ? 2 * rows * D : 0);
@@ -1288,9 +1385,10 @@ cudaError_t run(const KvAttendArgs& a, const KvPlan& p, const CUtensorMap* m, cu
   if (regs * 3 < 2 * 208 + 88) return cudaErrorInvalidKernelImage;
   e = launch_after(k_kv_attend<D, HALF>, p.ctas, NT_ATT, L::SMEM, st, m[0], m[1], m[2], m[3], a, p);
   if (e != cudaSuccess) return e;
-  // a warp a row; no more than the GPU holds at once
-  const int64_t rows = std::max<int64_t>((int64_t)p.ctas * 256, a.b.n_groups ? (int64_t)a.b.n_tokens * a.n_heads : 0);
-  return launch_after(k_kv_join<D, HALF>, (unsigned)std::min<int64_t>((rows + 3) / 4, (int64_t)p.ctas * 8), 128, 0, st, a, p);
+  // no more CTAs than the GPU holds at once
+  const int64_t jobs = a.b.n_groups ? std::min<int64_t>(a.b.n_tokens / (2 * p.tpt) + a.b.n_groups, p.cap) : 0;
+  const int64_t tasks = (int64_t)p.ctas * 8 + jobs * a.c.n_kv_heads * 32;
+  return launch_after(k_kv_join<D, HALF>, (unsigned)std::min<int64_t>(tasks, (int64_t)p.ctas * 16), 256, 0, st, a, p);
 }
 
 }  // namespace
@@ -1317,7 +1415,7 @@ cudaError_t launch_kv_attend(const KvAttendArgs& a, void* ws, int32_t* err, int 
   if (!encode(&m[0], half, a.c.k, 4, ks, kst, kbox) || !encode(&m[1], half, a.c.v, 4, ks, kst, kbox) ||
       !encode(&m[2], half, a.q, 3, qs, qst, qbox) || !encode(&m[3], half, a.q, 3, qs, qst, qbox1))
     return cudaErrorInvalidValue;
-  const size_t psm = (size_t)(PLAN_JOBS + 1 + 4 * PLAN_GROUPS) * 8;
+  const size_t psm = (size_t)(PLAN_JOBS + 1 + 4 * PLAN_GROUPS) * 8 + (size_t)(3 * PLAN_GROUPS + 1) * 4;
   cudaError_t e = cudaFuncSetAttribute(k_kv_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)psm);
   if (e != cudaSuccess) return e;
   k_kv_plan<<<1, NT_PLAN, psm, st>>>(a.b, p, a.c.n_kv_heads);
