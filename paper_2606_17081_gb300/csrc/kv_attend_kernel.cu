@@ -70,8 +70,10 @@ struct KvHead {
   int32_t jobs, prefix_jobs;
 };
 
-struct KvStart {
+struct __align__(16) KvStart {
   int32_t job, head, off, reserved0;   // where a CTA's share begins
+  int64_t rem, reserved1;              // its cost
+  KvJob j;                             // that job
 };
 
 struct KvPlan {
@@ -345,7 +347,7 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
   if (tid == 0) *p.head = KvHead{all, per, J, prefix_jobs};
   for (int c = tid; c < p.ctas; c += NT_PLAN) {
     const int64_t u = c * per;
-    KvStart s{0, 0, 0, 0};
+    KvStart s = {};
     KvCut cut = {};
     if (u < all) {
       int lo = 0, hi = J;   // the last job that starts at or before u
@@ -360,6 +362,8 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
       s.job = lo;
       s.head = (int)quotient(in, cj);
       s.off = (int)(in - (int64_t)s.head * cj);
+      s.rem = min(per, all - u);
+      s.j = j;
       const int64_t u0 = u - s.off;
       if (s.off > 0 && j.nt > 0 && (j.flags & JOB_ALONE) && u0 >= u - per) {   // not cut before
         const int w = tile_cost(j.flags);
@@ -531,13 +535,7 @@ __device__ __forceinline__ float row_max(uint32_t ts, bool cut, int left) {
   return fmaxf(m, n);
 }
 
-// The row's weights exp2(sl s + nm), packed into v's first half, and their sums
-// (of even and odd keys).
-template <bool HALF>
-__device__ __forceinline__ void row_exp(uint32_t ts, bool cut, int left, float sl, float nm, uint32_t* v,
-                                        float& a0, float& a1) {
-  float b0 = 0.0f, b1 = 0.0f;
-  a0 = a1 = 0.0f;
+__device__ __forceinline__ void row_load(uint32_t ts, bool cut, int left, uint32_t* v) {
 #pragma unroll
   for (int c = 0; c < 128; c += 32) tm_ld32(v + c, ts + c);
 #pragma unroll
@@ -546,6 +544,14 @@ __device__ __forceinline__ void row_exp(uint32_t ts, bool cut, int left, float s
 #pragma unroll
     for (int c = 0; c < 128; c += 32) cut32(v + c, left - c);
   }
+}
+
+// The row's weights exp2(sl s + nm), packed into v's first half, and their sums
+// (of even and odd keys).
+template <bool HALF>
+__device__ __forceinline__ void row_exp(float sl, float nm, uint32_t* v, float& a0, float& a1) {
+  float b0 = 0.0f, b1 = 0.0f;
+  a0 = a1 = 0.0f;
 #pragma unroll
   for (int k = 0; k < 128; k += 4) {
     float e0 = __uint_as_float(v[k]), e1 = __uint_as_float(v[k + 1]), e2 = __uint_as_float(v[k + 2]),
@@ -599,15 +605,13 @@ struct Walk {
   Seg a, b;
 
   __device__ Walk(const KvPlan& p, int n_kv_heads) {
-    const KvHead hd = *p.head;
-    const int64_t u = (int64_t)blockIdx.x * hd.per;
+    const KvStart s = p.start[blockIdx.x];
     jobs = p.jobs;
     heads = n_kv_heads;
-    rem = min(hd.per, hd.total - u);
-    const KvStart s = p.start[blockIdx.x];
+    rem = s.rem;
     j = s.job; h = s.head; off = s.off;
+    ahead = s.j;
     held = false;
-    if (rem > 0) ahead = jobs[j];
   }
   __device__ bool pull(Seg& s) {
     while (rem > 0) {
@@ -661,6 +665,8 @@ struct Walk {
   }
 };
 
+constexpr int NR = 4;   // runs ahead
+
 template <int D>
 struct Lay {
   static constexpr int QSLOT = 128 * D * 2;       // bytes of 128 rows
@@ -668,11 +674,11 @@ struct Lay {
   static constexpr int NST = D == 128 ? 5 : 12;   // stages: what 227 KB leave beside the rows
   static constexpr int RING = 2 * QSLOT;
   static constexpr int MISC = RING + NST * STAGE;
-  // barriers: full[NST], empty[NST], qfull[2], qempty[2], sfull[2], pfull[2], ofull[2], oempty[2], rfull[2], rempty[2], meet
-  static constexpr int NBAR = 2 * NST + 17;
-  static constexpr int ML = MISC + 384;           // float2 [2][128]
-  static constexpr int RUNS = ML + 2048;          // Run [2]
-  static constexpr int SMEM = RUNS + 2 * (int)sizeof(Run);
+  // barriers: full[NST], empty[NST], qfull[2], qempty[2], sfull[2], pfull[2], ofull[2], oempty[2], meet, rfull[NR], rempty[NR]
+  static constexpr int NBAR = 2 * NST + 13 + 2 * NR;
+  static constexpr int ML = MISC + 384;           // float2 [128]
+  static constexpr int RUNS = ML + 1024;          // Run [NR]
+  static constexpr int SMEM = RUNS + NR * (int)sizeof(Run);
 };
 
 // The loads' order is that of first use: K of each stream's first tile, then for
@@ -688,9 +694,10 @@ __device__ __forceinline__ int vplace(int s, int i, int n0, int n1) {
 // under the other's products.  Warps 0-3 and 4-7 are the streams' softmax, a thread a row; warp 8 issues the products and
 // warp 9 the loads.
 // TMEM: S of each stream 128 columns (P, 64 columns, overwrites it), O D each.
-// The m of a row is the largest score of its first tile and moves only when a
-// tile's weights sum to more than 2^15 (each is then below it, in range of
-// fp16), which hardly happens: O and l are scaled then.
+// The m of a row is the largest score of its first 33 keys and moves only when a
+// tile's weights sum to more than 2^15 (up to there each is in range of fp16, and
+// bf16 weights are as exact at any size), which hardly happens: O and l are
+// scaled then.
 template <int D, bool HALF>
 __global__ void __launch_bounds__(NT_ATT, 1)
 k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
@@ -703,7 +710,7 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
   const uint32_t bars = base + L::MISC;
   const uint32_t FULL = bars, EMPTY = bars + 8 * L::NST, QFULL = bars + 16 * L::NST, QEMPTY = QFULL + 16,
                  SFULL = QFULL + 32, PFULL = QFULL + 48, OFULL = QFULL + 64, OEMPTY = QFULL + 80,
-                 RFULL = QFULL + 96, REMPTY = QFULL + 112, MEET = QFULL + 128;
+                 MEET = QFULL + 96, RFULL = QFULL + 104, REMPTY = RFULL + 8 * NR;
   Run* const runs = reinterpret_cast<Run*>(sm + L::RUNS);
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(sm + L::MISC + 8 * L::NBAR);
   volatile int* lost = reinterpret_cast<volatile int*>(sm + L::MISC + 8 * L::NBAR + 4);
@@ -722,10 +729,9 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
       mbar_init(PFULL + 8 * s, 4);
       mbar_init(OFULL + 8 * s, 1);
       mbar_init(OEMPTY + 8 * s, 4);
-      mbar_init(RFULL + 8 * s, 1);
-      mbar_init(REMPTY + 8 * s, 10);
     }
-    mbar_init(MEET, 8);
+    for (int s = 0; s < NR; s++) { mbar_init(RFULL + 8 * s, 1); mbar_init(REMPTY + 8 * s, 10); }
+    mbar_init(MEET, 4);
     *lost = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -756,8 +762,8 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
         if (w.kind <= RUN_PAIR && t < g.t1 && pg < (g.job.kend + 15) / 16)
           id = a.b.table[(int64_t)g.job.row * a.b.table_stride + pg];
         if (id < 0 || id >= a.c.n_blocks) id = (int)a.c.n_blocks;   // reads as zeros
-        if (k >= 2) mbar_wait(REMPTY + 8 * (k & 1), ((k >> 1) - 1) & 1, lost, p.err);
-        Run* const r = runs + (k & 1);
+        if (k >= NR) mbar_wait(REMPTY + 8 * (k % NR), (k / NR - 1) & 1, lost, p.err);
+        Run* const r = runs + k % NR;
         r->page[lane] = id;
         if (lane == 0) {
           const int n = w.a.nt();
@@ -768,15 +774,15 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
           r->n[1] = w.kind == RUN_SPLIT ? n >> 1 : w.kind == RUN_PAIR ? w.b.nt() : n;
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(RFULL + 8 * (k & 1));
+        if (lane == 0) mbar_arrive(RFULL + 8 * (k % NR));
         if (w.kind == RUN_END) break;
       }
     } else if (warp == 9) {
       // ---------------- loads (the warp as one; one thread issues)
       uint32_t qn = 0, x = 0;   // Q slots used, tiles loaded
       for (uint32_t k = 0; !*lost; k++) {
-        mbar_wait(RFULL + 8 * (k & 1), (k >> 1) & 1, lost, p.err);
-        const Run& r = runs[k & 1];
+        mbar_wait(RFULL + 8 * (k % NR), (k / NR) & 1, lost, p.err);
+        const Run& r = runs[k % NR];
         const int kind = r.kind;
         if (kind == RUN_END) break;
         if (kind != RUN_NONE) {
@@ -847,7 +853,7 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
           }
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(REMPTY + 8 * (k & 1));
+        if (lane == 0) mbar_arrive(REMPTY + 8 * (k % NR));
       }
     } else if (warp == 8) {
       // ---------------- products (the warp as one; one thread issues)
@@ -865,10 +871,10 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
         return st;
       };
       for (uint32_t k = 0; !*lost; k++) {
-        mbar_wait(RFULL + 8 * (k & 1), (k >> 1) & 1, lost, p.err);
-        const int kind = runs[k & 1].kind, n0 = runs[k & 1].n[0], n1 = runs[k & 1].n[1];
+        mbar_wait(RFULL + 8 * (k % NR), (k / NR) & 1, lost, p.err);
+        const int kind = runs[k % NR].kind, n0 = runs[k % NR].n[0], n1 = runs[k % NR].n[1];
         __syncwarp();
-        if (lane == 0) mbar_arrive(REMPTY + 8 * (k & 1));
+        if (lane == 0) mbar_arrive(REMPTY + 8 * (k % NR));
         if (kind == RUN_END) break;
         if (kind == RUN_NONE) continue;
         const bool wide = kind == RUN_WIDE, split = kind == RUN_SPLIT;
@@ -925,18 +931,12 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
     const uint32_t ts = tmem + lanes + s * 128;
     const float sl = __fmul_rn(a.scale, 1.4426950408889634f);
     float2* ml = reinterpret_cast<float2*>(sm + L::ML);
-    uint32_t ns = 0, no0 = 0, no1 = 0, loads = 0;
+    uint32_t ns = 0, nm = 0, no0 = 0, no1 = 0, loads = 0;
     const int tl = r / p.ratio, hl = r - tl * p.ratio;   // the row's token and head in its 128
     const int64_t all = (int64_t)a.b.n_tokens * a.n_heads;
-    uint32_t nm = 0;
-    auto meet = [&]() {   // of both streams' warps
-      __syncwarp();
-      if (lane == 0) mbar_arrive(MEET);
-      mbar_wait(MEET, nm++ & 1, lost, p.err);
-    };
     for (uint32_t k = 0;; k++) {
-      mbar_wait(RFULL + 8 * (k & 1), (k >> 1) & 1, lost, p.err);
-      const Run& run = runs[k & 1];
+      mbar_wait(RFULL + 8 * (k % NR), (k / NR) & 1, lost, p.err);
+      const Run& run = runs[k % NR];
       const int kind = run.kind;
       if (kind == RUN_END || *lost) break;
       const bool wide = kind == RUN_WIDE, split = kind == RUN_SPLIT;
@@ -952,7 +952,7 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
           if (a.lse) a.lse[(int64_t)row * a.n_heads + hq] = -INFINITY;
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(REMPTY + 8 * (k & 1));
+        if (lane == 0) mbar_arrive(REMPTY + 8 * (k % NR));
         continue;
       }
       const int n0 = run.n[0], n1 = run.n[1], n = s ? n1 : n0;
@@ -988,14 +988,16 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
           const bool cut = low < k0 + TK;   // (the warp's rows see different ends)
           const int left = lim - k0;
           const bool first = i == 0;   // O holds nothing yet
-          if (first) {
-            const float x = row_max(ts, cut, left);
-            if (live) m = x;
-          }
           uint32_t pk[128];
           float a0, a1;
           for (;;) {
-            row_exp<HALF>(ts, cut, left, sl, m == -INFINITY ? 0.0f : -__fmul_rn(m, sl), pk, a0, a1);
+            row_load(ts, cut, left, pk);
+            if (first && m == -INFINITY) {   // the largest of the first keys will do
+              m = __uint_as_float(pk[0]);
+#pragma unroll
+              for (int c = 1; c < 33; c += 2) m = max3(m, pk[c], pk[c + 1]);
+            }
+            row_exp<HALF>(sl, m == -INFINITY ? 0.0f : -__fmul_rn(m, sl), pk, a0, a1);
             const bool over = live && __fadd_rn(a0, a1) > 32768.0f, none = m == -INFINITY && left > 0;
             if (!__any_sync(~0u, over || none)) break;
             const float x = row_max(ts, cut, left);
@@ -1039,81 +1041,87 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
         if (lane == 0) mbar_arrive(PFULL + 8 * s);
       }
       loads += 2 * (n0 + (wide ? 0 : n1));
-      // ---- the rows' results: the stream's own, or both streams' joined, half the columns each
-      float l = __fadd_rn(l0, l1);
-      float f0, f1 = 0.0f, lse2;
-      int c0 = 0, c1 = D;
-      if (!split) {
-        f0 = l > 0.0f ? __fdiv_rn(1.0f, l) : l == l ? 0.0f : l;
-        lse2 = l > 0.0f ? __fadd_rn(__fmul_rn(m, sl), __log2f(l)) : l == l ? -INFINITY : l;
-        mbar_wait(OFULL + 8 * s, (s ? no1 : no0) & 1, lost, p.err);
-      } else {
-        ml[s * 128 + r] = make_float2(m, l);
-        meet();
-        const float2 x = ml[r], y = ml[128 + r];
-        const float mm = n1 > 0 ? fmaxf(x.x, y.x) : x.x;
-        const float wx = x.x == -INFINITY ? 0.0f : ex2(__fmul_rn(__fsub_rn(x.x, mm), sl));
-        const float wy = n1 == 0 || y.x == -INFINITY ? 0.0f : ex2(__fmul_rn(__fsub_rn(y.x, mm), sl));
-        l = fmaf(x.y, wx, __fmul_rn(y.y, wy));
-        const float inv = l > 0.0f ? __fdiv_rn(1.0f, l) : l == l ? 0.0f : l;
-        f0 = __fmul_rn(wx, inv);
-        f1 = __fmul_rn(wy, inv);
-        lse2 = l > 0.0f ? __fadd_rn(__fmul_rn(mm, sl), __log2f(l)) : l == l ? -INFINITY : l;
-        c0 = s * (D / 2);
-        c1 = c0 + D / 2;
-        mbar_wait(OFULL, no0 & 1, lost, p.err);
-        if (n1 > 0) mbar_wait(OFULL + 8, no1 & 1, lost, p.err);
+      // ---- the rows' results: each stream's own; of a split job both streams', by stream 0's warps
+      const bool mine = !split || s == 0;
+      float l = __fadd_rn(l0, l1), f1 = 0.0f;
+      if (n > 0) mbar_wait(OFULL + 8 * s, (s ? no1 : no0) & 1, lost, p.err);
+      if (split && n1 > 0) {
+        if (s) {   // (stream 0 is done with the row before, or this product could not have begun)
+          ml[r] = make_float2(m, l);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(MEET);
+        } else {
+          mbar_wait(MEET, nm++ & 1, lost, p.err);
+          mbar_wait(OFULL + 8, no1 & 1, lost, p.err);
+          const float2 y = ml[r];
+          const float mm = fmaxf(m, y.x);
+          const float wx = m == -INFINITY ? 0.0f : ex2(__fmul_rn(__fsub_rn(m, mm), sl));
+          f1 = y.x == -INFINITY ? 0.0f : ex2(__fmul_rn(__fsub_rn(y.x, mm), sl));
+          l = fmaf(l, wx, __fmul_rn(y.y, f1));
+          l0 = wx;
+          m = mm;
+        }
       }
       no0 += n0 > 0;
       no1 += n1 > 0;
       tc_after();
-      const bool whole = g.t0 == 0 && g.t1 == job.nt;
-      const bool direct = whole && (job.flags & JOB_ALONE);
-      if (any) {
+      if (any && mine) {
+        const float inv = l > 0.0f ? __fdiv_rn(1.0f, l) : l == l ? 0.0f : l;
+        const float f0 = split && n1 > 0 ? __fmul_rn(l0, inv) : inv;
+        const float lse2 = l > 0.0f ? __fadd_rn(__fmul_rn(m, sl), __log2f(l)) : l == l ? -INFINITY : l;
+        f1 = __fmul_rn(f1, inv);
+        const bool whole = g.t0 == 0 && g.t1 == job.nt;
+        const bool direct = whole && (job.flags & JOB_ALONE);
         // a part's row: with the other whole parts of all rows, or with the CTA's cut ones
         uint16_t* out = static_cast<uint16_t*>(a.out) + row * a.o_ts + hq * a.o_hs;
         const int64_t at = whole ? ((job.flags & JOB_PREFIX) ? 0 : all) + (int64_t)row * a.n_heads + hq
                                  : ((int64_t)blockIdx.x * 2 + (g.cut_front ? 0 : 1)) * 256 + (wide ? s * 128 : 0) + r;
         float* part = (whole ? p.home : p.part) + at * D;
-        if (live && c0 == 0) {
+        if (live) {
           if (!direct) (whole ? p.home_lse : p.part_lse)[at] = lse2;
           else if (a.lse) a.lse[(int64_t)row * a.n_heads + hq] = __fmul_rn(lse2, 0.6931471805599453f);
         }
 #pragma unroll 1
-        for (int c = c0; c < c1; c += 32) {
-          uint32_t o[32];
-          float y[32];
-          tm_ld32(o, tmem + lanes + 256 + (split ? 0 : s * D) + c);
+        for (int c = 0; c < D; c += 64) {
+          uint32_t o[64];
+          float y[64];
+          const uint32_t to = tmem + lanes + 256 + c;
+          tm_ld32(o, to + (split ? 0 : s * D));
+          tm_ld32(o + 32, to + (split ? 0 : s * D) + 32);
           tm_wait_ld(o);
+          tm_wait_ld(o + 32);
 #pragma unroll
-          for (int k = 0; k < 32; k++) y[k] = f0 == 0.0f ? 0.0f : __fmul_rn(__uint_as_float(o[k]), f0);
+          for (int k = 0; k < 64; k++) y[k] = f0 == 0.0f ? 0.0f : __fmul_rn(__uint_as_float(o[k]), f0);
           if (split && n1 > 0) {
-            tm_ld32(o, tmem + lanes + 256 + D + c);
+            tm_ld32(o, to + D);
+            tm_ld32(o + 32, to + D + 32);
             tm_wait_ld(o);
+            tm_wait_ld(o + 32);
 #pragma unroll
-            for (int k = 0; k < 32; k++) y[k] = f1 == 0.0f ? y[k] : fmaf(__uint_as_float(o[k]), f1, y[k]);
+            for (int k = 0; k < 64; k++) y[k] = f1 == 0.0f ? y[k] : fmaf(__uint_as_float(o[k]), f1, y[k]);
           }
           if (live) {
             if (direct) {
 #pragma unroll
-              for (int k = 0; k < 32; k += 8)
+              for (int k = 0; k < 64; k += 8)
                 *reinterpret_cast<uint4*>(out + c + k) =
                     make_uint4(pack2<HALF>(y[k], y[k + 1]), pack2<HALF>(y[k + 2], y[k + 3]),
                                pack2<HALF>(y[k + 4], y[k + 5]), pack2<HALF>(y[k + 6], y[k + 7]));
             } else {
 #pragma unroll
-              for (int k = 0; k < 32; k += 4)
+              for (int k = 0; k < 64; k += 4)
                 *reinterpret_cast<float4*>(part + c + k) = make_float4(y[k], y[k + 1], y[k + 2], y[k + 3]);
             }
           }
         }
       }
       tc_before();
-      if (split) meet();   // ml and both O are free again
       __syncwarp();
       if (lane == 0) {
-        mbar_arrive(OEMPTY + 8 * s);
-        mbar_arrive(REMPTY + 8 * (k & 1));
+        // (a split job's O of stream 1 is stream 0's to give back)
+        if (mine) mbar_arrive(OEMPTY + 8 * s);
+        if (split && mine) mbar_arrive(OEMPTY + 8);
+        mbar_arrive(REMPTY + 8 * (k % NR));
       }
     }
   }
