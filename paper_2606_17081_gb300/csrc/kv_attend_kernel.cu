@@ -32,7 +32,7 @@ constexpr int TK = 128;        // keys of a tile
 // Costs: a tile of a job of at most 128 rows, one of a larger job, and a job's
 // own (its rows' loads and stores).
 constexpr int W_NARROW = 2, W_WIDE = 3, OV = 2;
-constexpr int NT_PLAN = 1024;
+constexpr int NT_PLAN = 1024;   // at most: 256 where that is a thread a request
 constexpr int NT_ATT = 384;
 constexpr int PLAN_GROUPS = 1024;   // groups whose sums are kept in shared memory
 constexpr int PLAN_JOBS = 4096;     // jobs whose costs are
@@ -58,7 +58,7 @@ struct __align__(16) KvJob {
 
 // A job and head that a share's end cuts, at the share's end that cuts it first.
 struct __align__(16) KvCut {
-  int32_t tok0, ntok;   // (ntok 0: none)
+  int32_t tok0, ntok;
   int32_t head;
   int32_t c0;           // the CTA in which it begins
   int32_t first, last;  // CTAs that have tiles of it
@@ -67,7 +67,7 @@ struct __align__(16) KvCut {
 
 struct KvHead {
   int64_t total, per;   // cost of all jobs and heads, of one CTA
-  int32_t jobs, prefix_jobs;
+  int32_t jobs, prefix_jobs, cuts, reserved0;
 };
 
 struct __align__(16) KvStart {
@@ -83,7 +83,7 @@ struct KvPlan {
   int32_t* gjob;        // [n_groups] first prefix job, -1: not shared (more than PLAN_GROUPS groups)
   unsigned long long* gsum;   // [4 n_groups] (more than PLAN_GROUPS groups)
   KvStart* start;       // [ctas]
-  KvCut* cut;           // [ctas]
+  KvCut* cut;           // [ctas] the cut jobs, in any order
   float* part;          // [ctas][2][256][D] cut jobs' rows: of the first cut job (0), of the last (1)
   float* part_lse;      // [ctas][2][256]
   float* home;          // [2][rows][D] rows with a prefix job and an own one, each whole
@@ -115,7 +115,7 @@ __device__ int64_t block_scan(int64_t x, int64_t* sm, int64_t* total) {
   __syncthreads();   // (sm may still be read from the scan before)
   if (lane == 31) sm[warp] = s;
   __syncthreads();
-  int64_t w = lane < NT_PLAN / 32 ? sm[lane] : 0, ws = w;
+  int64_t w = lane < (blockDim.x >> 5) ? sm[lane] : 0, ws = w;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int64_t y = __shfl_up_sync(~0u, ws, o);
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
   int32_t* s_prefix = s_start + PLAN_GROUPS + 1;                 // [PLAN_GROUPS]
   int32_t* s_gjob = s_prefix + PLAN_GROUPS;                      // [PLAN_GROUPS]
   __shared__ int64_t s_scan[NT_PLAN / 32];
-  const int tid = threadIdx.x, n = b.n_req, G = b.n_groups;
+  const int tid = threadIdx.x, nt = blockDim.x, n = b.n_req, G = b.n_groups;
   const int w2 = 2 * p.tpt;
   const bool few = G <= PLAN_GROUPS;
   unsigned long long* sum = few ? s_sum : p.gsum;
@@ -199,12 +199,12 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
   if (tid < n) mine = lens(tid);
   const int q_end = n > 0 ? rows_at(n) : 0;
   if (few && G > 0) {
-    for (int g = tid; g <= G; g += NT_PLAN) s_start[g] = b.group_start[g];
-    for (int g = tid; g < G; g += NT_PLAN) s_prefix[g] = b.prefix_len[g];
+    for (int g = tid; g <= G; g += nt) s_start[g] = b.group_start[g];
+    for (int g = tid; g < G; g += nt) s_prefix[g] = b.prefix_len[g];
   }
   // of each group: its requests' costs without and with a shared prefix, whether
   // some row sees less than the prefix, the longest context
-  for (int x = tid; x < 4 * G; x += NT_PLAN) sum[x] = 0;
+  for (int x = tid; x < 4 * G; x += nt) sum[x] = 0;
   __syncthreads();
   mine.g = tid < n ? group(tid) : -1;
   auto request = [&](int i) {
@@ -214,16 +214,23 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
     return r;
   };
   if (G > 0) {
-    for (int i = tid; i < n; i += NT_PLAN) {
+    for (int i = tid; i < n; i += nt) {
       const ReqLens r = request(i);
       const int g = r.g;
       if (g < 0 || r.q == 0) continue;
       const int P = prefix_keys(g), rt = (r.q + w2 - 1) / w2, seen = r.kv - (r.q >> 1);
       const int fl = r.q > p.tpt ? JOB_WIDE : 0;
-      atomicAdd(&sum[4 * g], (unsigned long long)rt * job_cost(tiles(seen), fl));
-      atomicAdd(&sum[4 * g + 1], (unsigned long long)rt * job_cost(tiles(seen - P), fl));
-      if (r.kv - r.q + 1 < P) sum[4 * g + 2] = 1;
-      atomicMax(&sum[4 * g + 3], (unsigned long long)r.kv);
+      // (a warp's requests of one group together; 2^26 a request is more than any step holds)
+      const unsigned top = 1u << 26, peers = __match_any_sync(__activemask(), g);
+      const unsigned apart = __reduce_add_sync(peers, (unsigned)min((int64_t)rt * job_cost(tiles(seen), fl), (int64_t)top));
+      const unsigned with = __reduce_add_sync(peers, (unsigned)min((int64_t)rt * job_cost(tiles(seen - P), fl), (int64_t)top));
+      const unsigned less = __reduce_or_sync(peers, r.kv - r.q + 1 < P), most = __reduce_max_sync(peers, (unsigned)r.kv);
+      if ((tid & 31) == __ffs(peers) - 1) {
+        atomicAdd(&sum[4 * g], (unsigned long long)apart);
+        atomicAdd(&sum[4 * g + 1], (unsigned long long)with);
+        if (less) sum[4 * g + 2] = 1;
+        atomicMax(&sum[4 * g + 3], (unsigned long long)most);
+      }
     }
     __syncthreads();
   }
@@ -237,7 +244,7 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
   // through memory (2 parts written and read, 4 D bytes each a row, against
   // 512 D bytes a tile).
   int64_t jobs = 0, total;
-  for (int base = 0; base < G; base += NT_PLAN) {
+  for (int base = 0; base < G; base += nt) {
     const int g = base + tid;
     int cnt = 0, t0 = 0, t1 = 0, P = 0, first = 0;
     if (g < G) {
@@ -275,7 +282,7 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
   const int prefix_jobs = (int)jobs;
   __syncthreads();   // gjob
   // the requests' own jobs
-  for (int base = 0; base < n; base += NT_PLAN) {
+  for (int base = 0; base < n; base += nt) {
     const int i = base + tid;
     ReqLens r{0, 0, 0, -1};
     int key0 = 0, cnt = 0;
@@ -319,7 +326,7 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
   }
   // rows of no request: jobs without keys
   const int pads = (b.n_tokens - q_end + w2 - 1) / w2;
-  for (int k = tid; k < pads; k += NT_PLAN) {
+  for (int k = tid; k < pads; k += nt) {
     KvJob j = {};
     j.tok0 = q_end + k * w2;
     j.ntok = min(w2, b.n_tokens - j.tok0);
@@ -329,7 +336,7 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
   const int J = (int)min(jobs + pads, (int64_t)p.cap);
   __syncthreads();   // the jobs
   int64_t cost = 0;
-  for (int base = 0; base < J; base += NT_PLAN) {
+  for (int base = 0; base < J; base += nt) {
     const int j = base + tid;
     int64_t c = 0;
     if (j < J) c = j < PLAN_JOBS ? s_cost[j] : job_cost(p.jobs[j].nt, p.jobs[j].flags);
@@ -344,8 +351,10 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
   const int64_t all = cost * n_kv_heads;
   // two tiles at least, one for each stream of a CTA
   const int64_t per = max((all + p.ctas - 1) / p.ctas, (int64_t)(2 * W_NARROW + OV));
-  if (tid == 0) *p.head = KvHead{all, per, J, prefix_jobs};
-  for (int c = tid; c < p.ctas; c += NT_PLAN) {
+  __shared__ int s_cuts;
+  if (tid == 0) s_cuts = 0;
+  __syncthreads();
+  for (int c = tid; c < p.ctas; c += nt) {
     const int64_t u = c * per;
     KvStart s = {};
     KvCut cut = {};
@@ -373,12 +382,14 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
         cut.last = segment(u0, cj, w, j.nt, per, e, t0, t1) ? e : e - 1;
         cut.tok0 = j.tok0;
         cut.head = s.head;
-        cut.ntok = cut.first < cut.last ? j.ntok : 0;   // (else whole in one CTA)
+        cut.ntok = j.ntok;
+        if (cut.first < cut.last) p.cut[atomicAdd(&s_cuts, 1)] = cut;   // (else whole in one CTA)
       }
     }
     p.start[c] = s;
-    p.cut[c] = cut;
   }
+  __syncthreads();
+  if (tid == 0) *p.head = KvHead{all, per, J, prefix_jobs, s_cuts, 0};
 }
 
 // ------------------------------------------------------------------ PTX
@@ -489,6 +500,10 @@ __device__ __forceinline__ void fma2(float& x, float& y, float a, float b) {   /
   asm("{\n\t.reg .b64 s, t, u;\n\tmov.b64 s, {%0, %1};\n\tmov.b64 t, {%2, %2};\n\tmov.b64 u, {%3, %3};\n\t"
       "fma.rn.f32x2 s, s, t, u;\n\tmov.b64 {%0, %1}, s;\n\t}" : "+f"(x), "+f"(y) : "f"(a), "f"(b));
 }
+__device__ __forceinline__ void mul2(float& x, float& y, float a) {
+  asm("{\n\t.reg .b64 s, t;\n\tmov.b64 s, {%0, %1};\n\tmov.b64 t, {%2, %2};\n\t"
+      "mul.rn.f32x2 s, s, t;\n\tmov.b64 {%0, %1}, s;\n\t}" : "+f"(x), "+f"(y) : "f"(a));
+}
 __device__ __forceinline__ void add2(float& x, float& y, float a, float b) {
   asm("{\n\t.reg .b64 s, t;\n\tmov.b64 s, {%0, %1};\n\tmov.b64 t, {%2, %3};\n\t"
       "add.rn.f32x2 s, s, t;\n\tmov.b64 {%0, %1}, s;\n\t}" : "+f"(x), "+f"(y) : "f"(a), "f"(b));
@@ -515,17 +530,16 @@ __device__ __forceinline__ float max3(float a, uint32_t b, uint32_t c) {
   return r;
 }
 
-// The largest score of a row's tile.
-__device__ __forceinline__ float row_max(uint32_t ts, bool cut, int left) {
-  uint32_t v[2][32];
+// The largest score of a row's tile, of which the warp's rows see `seen` keys at
+// most and this one `left`.
+__device__ __noinline__ float row_max(uint32_t ts, int seen, int left) {
   float m = -INFINITY, n = -INFINITY;
-  tm_ld32(v[0], ts);
-#pragma unroll
-  for (int c = 0; c < 4; c++) {
-    uint32_t* x = v[c & 1];
+#pragma unroll 1
+  for (int c = 0; c < min(seen, TK); c += 32) {
+    uint32_t x[32];
+    tm_ld32(x, ts + c);
     tm_wait_ld(x);
-    if (c < 3) tm_ld32(v[(c + 1) & 1], ts + 32 * (c + 1));
-    if (cut) cut32(x, left - 32 * c);
+    cut32(x, left - c);
 #pragma unroll
     for (int k = 0; k < 32; k += 4) {
       m = max3(m, x[k], x[k + 1]);
@@ -535,25 +549,23 @@ __device__ __forceinline__ float row_max(uint32_t ts, bool cut, int left) {
   return fmaxf(m, n);
 }
 
-__device__ __forceinline__ void row_load(uint32_t ts, bool cut, int left, uint32_t* v) {
+__device__ __forceinline__ float max_of32(const uint32_t* v) {
+  float m = __uint_as_float(v[0]), n = __uint_as_float(v[31]);
 #pragma unroll
-  for (int c = 0; c < 128; c += 32) tm_ld32(v + c, ts + c);
-#pragma unroll
-  for (int c = 0; c < 128; c += 32) tm_wait_ld(v + c);
-  if (cut) {
-#pragma unroll
-    for (int c = 0; c < 128; c += 32) cut32(v + c, left - c);
+  for (int k = 1; k < 29; k += 4) {
+    m = max3(m, v[k], v[k + 1]);
+    n = max3(n, v[k + 2], v[k + 3]);
   }
+  return fmaxf(max3(m, v[29], v[30]), n);
 }
 
-// The row's weights exp2(sl s + nm), packed into v's first half, and their sums
-// (of even and odd keys).
-template <bool HALF>
+// Weights exp2(sl s + nm) of 4 N scores, packed in pairs into v's first half, and
+// added to the sums of even and odd keys.
+template <bool HALF, int N>
 __device__ __forceinline__ void row_exp(float sl, float nm, uint32_t* v, float& a0, float& a1) {
   float b0 = 0.0f, b1 = 0.0f;
-  a0 = a1 = 0.0f;
 #pragma unroll
-  for (int k = 0; k < 128; k += 4) {
+  for (int k = 0; k < 4 * N; k += 4) {
     float e0 = __uint_as_float(v[k]), e1 = __uint_as_float(v[k + 1]), e2 = __uint_as_float(v[k + 2]),
           e3 = __uint_as_float(v[k + 3]);
     fma2(e0, e1, sl, nm);
@@ -566,6 +578,8 @@ __device__ __forceinline__ void row_exp(float sl, float nm, uint32_t* v, float& 
   }
   add2(a0, a1, b0, b1);
 }
+
+__device__ __forceinline__ float minus(float m, float sl) { return m == -INFINITY ? 0.0f : -__fmul_rn(m, sl); }
 
 // ------------------------------------------------------------------ the kernel
 
@@ -694,7 +708,7 @@ __device__ __forceinline__ int vplace(int s, int i, int n0, int n1) {
 // under the other's products.  Warps 0-3 and 4-7 are the streams' softmax, a thread a row; warp 8 issues the products and
 // warp 9 the loads.
 // TMEM: S of each stream 128 columns (P, 64 columns, overwrites it), O D each.
-// The m of a row is the largest score of its first 33 keys and moves only when a
+// The m of a row is the largest score of its first 32 keys and moves only when a
 // tile's weights sum to more than 2^15 (up to there each is in range of fp16, and
 // bf16 weights are as exact at any size), which hardly happens: O and l are
 // scaled then.
@@ -976,7 +990,7 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
       }
       // keys of a last tile that the job's end cuts
       const int ends = g.t1 == job.nt ? (job.kend - job.key0) & (TK - 1) : 0;
-      const int low = __reduce_min_sync(~0u, live ? lim : INT_MAX);
+      const int low = __reduce_min_sync(~0u, live ? lim : INT_MAX), high = __reduce_max_sync(~0u, live ? lim : 0);
       float m = live ? -INFINITY : 0.0f, l0 = 0.0f, l1 = 0.0f;
       for (int i = 0; i < n; i++) {
         const int t = split ? 2 * i + s : i;
@@ -984,27 +998,59 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
         ns++;
         tc_after();
         if (any) {
-          const int k0 = (g.t0 + t) * TK;
-          const bool cut = low < k0 + TK;   // (the warp's rows see different ends)
-          const int left = lim - k0;
+          const int k0 = (g.t0 + t) * TK, left = lim - k0, seen = high - k0;
           const bool first = i == 0;   // O holds nothing yet
-          uint32_t pk[128];
+          bool stuck = false;
           float a0, a1;
           for (;;) {
-            row_load(ts, cut, left, pk);
-            if (first && m == -INFINITY) {   // the largest of the first keys will do
-              m = __uint_as_float(pk[0]);
+            a0 = a1 = 0.0f;
+            // (m from a row's first keys will do)
+            if (low >= k0 + TK) {
+              uint32_t v[128];
 #pragma unroll
-              for (int c = 1; c < 33; c += 2) m = max3(m, pk[c], pk[c + 1]);
+              for (int c = 0; c < TK; c += 32) tm_ld32(v + c, ts + c);
+#pragma unroll
+              for (int c = 0; c < TK; c += 32) tm_wait_ld(v + c);
+              if (first && m == -INFINITY) m = max_of32(v);
+              row_exp<HALF, 32>(sl, minus(m, sl), v, a0, a1);
+              const bool over = live && __fadd_rn(a0, a1) > 32768.0f;
+              if (stuck || !__any_sync(~0u, over || m == -INFINITY)) {
+                tm_st32(ts, v);
+                tm_st32(ts + 32, v + 32);
+                break;
+              }
+            } else {
+              // the warp's rows see different ends: 32 keys at a time, up to the last that one sees
+              uint32_t w[64];
+#pragma unroll
+              for (int c = 0; c < 64; c++) w[c] = 0;
+#pragma unroll
+              for (int c = 0; c < TK; c += 32) {
+                if (c < seen) {
+                  uint32_t v[32];
+                  tm_ld32(v, ts + c);
+                  tm_wait_ld(v);
+                  cut32(v, left - c);
+                  if (c == 0 && first && m == -INFINITY) m = max_of32(v);
+                  row_exp<HALF, 8>(sl, minus(m, sl), v, a0, a1);
+#pragma unroll
+                  for (int k = 0; k < 16; k++) w[c / 2 + k] = v[k];
+                }
+              }
+              const bool over = live && __fadd_rn(a0, a1) > 32768.0f;
+              if (stuck || !__any_sync(~0u, over || (m == -INFINITY && left > 0))) {
+                tm_st32(ts, w);
+                tm_st32(ts + 32, w + 32);
+                break;
+              }
             }
-            row_exp<HALF>(sl, m == -INFINITY ? 0.0f : -__fmul_rn(m, sl), pk, a0, a1);
+            // a row's m moves: O and l are scaled
             const bool over = live && __fadd_rn(a0, a1) > 32768.0f, none = m == -INFINITY && left > 0;
-            if (!__any_sync(~0u, over || none)) break;
-            const float x = row_max(ts, cut, left);
+            const float x = row_max(ts, seen, left);
             const float m2 = over || none ? fmaxf(m, x) : m;
-            if (!__any_sync(~0u, m2 != m)) break;   // (an infinity: no larger m)
+            const bool moved = __any_sync(~0u, m2 != m);
             const float f = m == m2 ? 1.0f : ex2(__fmul_rn(__fsub_rn(m, m2), sl));
-            if (!first) {
+            if (!first && moved) {
               l0 = __fmul_rn(l0, f);
               l1 = __fmul_rn(l1, f);
 #pragma unroll 1
@@ -1018,9 +1064,8 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
               }
             }
             m = m2;
+            if (!moved) stuck = true;   // (an infinity: no larger m will do)
           }
-          tm_st32(ts, pk);
-          tm_st32(ts + 32, pk + 32);
           l0 = __fadd_rn(l0, a0);
           l1 = __fadd_rn(l1, a1);
           tm_wait_st();
@@ -1091,14 +1136,18 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
           tm_wait_ld(o);
           tm_wait_ld(o + 32);
 #pragma unroll
-          for (int k = 0; k < 64; k++) y[k] = f0 == 0.0f ? 0.0f : __fmul_rn(__uint_as_float(o[k]), f0);
+          for (int k = 0; k < 64; k += 2) {
+            y[k] = __uint_as_float(o[k]);
+            y[k + 1] = __uint_as_float(o[k + 1]);
+            mul2(y[k], y[k + 1], f0);
+          }
           if (split && n1 > 0) {
             tm_ld32(o, to + D);
             tm_ld32(o + 32, to + D + 32);
             tm_wait_ld(o);
             tm_wait_ld(o + 32);
 #pragma unroll
-            for (int k = 0; k < 64; k++) y[k] = f1 == 0.0f ? y[k] : fmaf(__uint_as_float(o[k]), f1, y[k]);
+            for (int k = 0; k < 64; k++) y[k] = fmaf(__uint_as_float(o[k]), f1, y[k]);
           }
           if (live) {
             if (direct) {
@@ -1207,12 +1256,13 @@ __device__ __forceinline__ void join_row(const KvAttendArgs& a, const KvPlan& p,
     for (int e = 0; e < E; e++) o[e] = __fmul_rn(o[e], f);
     m = m2;
     const int here = min(32, count - base);
-    for (int q = 0; q < here; q += 4) {
-      float w4[4], v[4][E];
+    for (int q = 0; q < here; q += 8) {
+      float w8[8], v[8][E];
 #pragma unroll
-      for (int z = 0; z < 4; z++) {   // (lanes past the last part have weight 0 and the first one's row)
+      for (int z = 0; z < 8; z++) {   // (past the last part: weight 0, the last one's row)
         const int from = min(q + z, here - 1);
-        w4[z] = q + z < here ? __shfl_sync(~0u, wt, from) : 0.0f;
+        const float w = __shfl_sync(~0u, wt, from);
+        w8[z] = q + z < here ? w : 0.0f;
         const float* r = reinterpret_cast<const float*>(__shfl_sync(~0u, reinterpret_cast<unsigned long long>(src), from)) + lane * E;
         if constexpr (E == 4) {
           const float4 t = *reinterpret_cast<const float4*>(r);
@@ -1223,9 +1273,9 @@ __device__ __forceinline__ void join_row(const KvAttendArgs& a, const KvPlan& p,
         }
       }
 #pragma unroll
-      for (int z = 0; z < 4; z++)
+      for (int z = 0; z < 8; z++)
 #pragma unroll
-        for (int e = 0; e < E; e++) o[e] = w4[z] == 0.0f ? o[e] : fmaf(w4[z], v[z][e], o[e]);
+        for (int e = 0; e < E; e++) o[e] = w8[z] == 0.0f ? o[e] : fmaf(w8[z], v[z][e], o[e]);
     }
   }
   const float inv = l == 0.0f ? 0.0f : __fdiv_rn(1.0f, l);
@@ -1239,69 +1289,63 @@ __device__ __forceinline__ void join_row(const KvAttendArgs& a, const KvPlan& p,
     a.lse[home] = l == 0.0f ? -INFINITY : __fmul_rn(__fadd_rn(m, __log2f(l)), 0.6931471805599453f);
 }
 
-// Rows that have parts, a warp a row: of the jobs that a share's end cut (a CTA
-// for 32 of the job's 256), and of shared groups, whose rows have a prefix job
-// and an own one (a CTA for 8).  The parts' order is the keys', so the result
-// does not depend on when they came.  What the plan says is read before the
-// attention kernel has ended (the plan had, when it let this one start).
+// Rows that have parts, a warp a row, a CTA for 8 of a job's 256: of the jobs that
+// a share's end cut, and of shared groups, whose rows have a prefix job and an own
+// one.  The parts' order is the keys', so the result does not depend on when they
+// came.  What the plan says is read before the attention kernel has ended (the
+// plan had, when it let this one start).
 template <int D, bool HALF>
 __global__ void __launch_bounds__(256) k_kv_join(const __grid_constant__ KvAttendArgs a,
                                                  const __grid_constant__ KvPlan p) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int hk = a.c.n_kv_heads, w2 = 2 * p.tpt, n = a.b.n_req;
+  KvHead hd;
+  const int4 h0 = __ldcg(reinterpret_cast<const int4*>(p.head)), h1 = __ldcg(reinterpret_cast<const int4*>(p.head) + 1);
+  memcpy(&hd, &h0, 16);
+  memcpy(reinterpret_cast<char*>(&hd) + 16, &h1, 16);
   bool waited = false;
   auto wait = [&]() {
     if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
     waited = true;
   };
-  const int cuts = p.ctas * 8;
-  int64_t task = blockIdx.x;
-  for (; task < cuts; task += gridDim.x) {
-    const int4* c = reinterpret_cast<const int4*>(p.cut + (task >> 3));
-    const int4 c0 = __ldcg(c), c1 = __ldcg(c + 1);
-    const int r0 = (int)(task & 7) * 32 + warp * 4, half = r0 >> 7;   // the warp's four rows
-    const Parts x{c0.w, c1.x, c1.y, c1.y - c1.x + 1}, none{0, 0, 0, 0};
-    for (int k = 0; k < 4; k++) {
-      const int r = (r0 & 127) + k, tl = r / p.ratio, tok = half * p.tpt + tl;
-      if (tl >= p.tpt || tok >= c0.y) break;
+  const int64_t cuts = (int64_t)hd.cuts * 32, tasks = cuts + (int64_t)hd.prefix_jobs * hk * 32;
+  for (int64_t task = blockIdx.x; task < tasks; task += gridDim.x) {
+    const int rr = (int)(task & 31) * 8 + warp, r = rr & 127, tl = r / p.ratio, hl = r - tl * p.ratio;
+    const int tok = (rr >> 7) * p.tpt + tl;
+    if (task < cuts) {
+      const int4* c = reinterpret_cast<const int4*>(p.cut + (task >> 5));
+      const int4 c0 = __ldcg(c), c1 = __ldcg(c + 1);
+      if (tl >= p.tpt || tok >= c0.y) continue;
+      const Parts x{c0.w, c1.x, c1.y, c1.y - c1.x + 1}, none{0, 0, 0, 0};
       wait();
-      join_row<D, HALF>(a, p, x, r0 + k, none, 0, (int64_t)c0.x + tok, c0.z * p.ratio + r - tl * p.ratio, lane);
+      join_row<D, HALF>(a, p, x, rr, none, 0, (int64_t)c0.x + tok, c0.z * p.ratio + hl, lane);
+      continue;
     }
-  }
-  if (a.b.n_groups > 0) {
-    KvHead hd;
-    const int4 h0 = __ldcg(reinterpret_cast<const int4*>(p.head)), h1 = __ldcg(reinterpret_cast<const int4*>(p.head) + 1);
-    memcpy(&hd, &h0, 16);
-    memcpy(reinterpret_cast<char*>(&hd) + 16, &h1, 8);
-    for (task -= cuts; task < (int64_t)hd.prefix_jobs * hk * 32; task += gridDim.x) {
-      const int pj = (int)((task >> 5) / hk), kh = (int)((task >> 5) - (int64_t)pj * hk);
-      const KvJob pre = job_from_l2(p.jobs + pj);
-      const int rr = (int)(task & 31) * 8 + warp, r = rr & 127, tl = r / p.ratio, hl = r - tl * p.ratio;
-      const int tok = (rr >> 7) * p.tpt + tl;
-      if (tl >= p.tpt || tok >= pre.ntok) continue;
-      const int row = pre.tok0 + tok;
-      int i = row;   // single tokens: request i has row i
-      if (!(row < n && __ldcg(a.b.q_start + row) == row && __ldcg(a.b.q_start + row + 1) == row + 1)) {
-        int lo = 0, hi = n;
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (__ldcg(a.b.q_start + mid) <= row) lo = mid; else hi = mid;
-        }
-        i = lo;
+    const int u = (int)((task - cuts) >> 5), pj = u / hk, kh = u - pj * hk;
+    const KvJob pre = job_from_l2(p.jobs + pj);
+    if (tl >= p.tpt || tok >= pre.ntok) continue;
+    const int row = pre.tok0 + tok;
+    int i = row;   // single tokens: request i has row i
+    if (!(row < n && __ldcg(a.b.q_start + row) == row && __ldcg(a.b.q_start + row + 1) == row + 1)) {
+      int lo = 0, hi = n;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (__ldcg(a.b.q_start + mid) <= row) lo = mid; else hi = mid;
       }
-      const int j0 = __ldcg(p.job0 + i), q0 = __ldcg(a.b.q_start + i);
-      Parts own{0, 0, 0, 0};
-      int ro = 0;
-      if (j0 >= 0 && q0 >= 0 && row >= q0) {
-        const KvJob j = job_from_l2(p.jobs + min(j0 + (row - q0) / w2, hd.jobs - 1));
-        const int t = row - j.tok0;
-        if (t >= 0 && t < j.ntok) own = parts_of(j, kh, hk, hd);
-        ro = (t >= p.tpt ? 128 + (t - p.tpt) * p.ratio : t * p.ratio) + hl;
-      }
-      const Parts x = parts_of(pre, kh, hk, hd);
-      wait();
-      join_row<D, HALF>(a, p, x, rr, own, ro, row, kh * p.ratio + hl, lane);
+      i = lo;
     }
+    const int j0 = __ldcg(p.job0 + i), q0 = __ldcg(a.b.q_start + i);
+    Parts own{0, 0, 0, 0};
+    int ro = 0;
+    if (j0 >= 0 && q0 >= 0 && row >= q0) {
+      const KvJob j = job_from_l2(p.jobs + min(j0 + (row - q0) / w2, hd.jobs - 1));
+      const int t = row - j.tok0;
+      if (t >= 0 && t < j.ntok) own = parts_of(j, kh, hk, hd);
+      ro = (t >= p.tpt ? 128 + (t - p.tpt) * p.ratio : t * p.ratio) + hl;
+    }
+    const Parts x = parts_of(pre, kh, hk, hd);
+    wait();
+    join_row<D, HALF>(a, p, x, rr, own, ro, row, kh * p.ratio + hl, lane);
   }
   wait();   // (no CTA ends before the attention kernel: the next call's plan waits for this one)
 }
@@ -1395,7 +1439,7 @@ cudaError_t run(const KvAttendArgs& a, const KvPlan& p, const CUtensorMap* m, cu
   if (e != cudaSuccess) return e;
   // no more CTAs than the GPU holds at once
   const int64_t jobs = a.b.n_groups ? std::min<int64_t>(a.b.n_tokens / (2 * p.tpt) + a.b.n_groups, p.cap) : 0;
-  const int64_t tasks = (int64_t)p.ctas * 8 + jobs * a.c.n_kv_heads * 32;
+  const int64_t tasks = (p.ctas + jobs * a.c.n_kv_heads) * 32;
   return launch_after(k_kv_join<D, HALF>, (unsigned)std::min<int64_t>(tasks, (int64_t)p.ctas * 16), 256, 0, st, a, p);
 }
 
@@ -1426,7 +1470,7 @@ cudaError_t launch_kv_attend(const KvAttendArgs& a, void* ws, int32_t* err, int 
   const size_t psm = (size_t)(PLAN_JOBS + 1 + 4 * PLAN_GROUPS) * 8 + (size_t)(3 * PLAN_GROUPS + 1) * 4;
   cudaError_t e = cudaFuncSetAttribute(k_kv_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)psm);
   if (e != cudaSuccess) return e;
-  k_kv_plan<<<1, NT_PLAN, psm, st>>>(a.b, p, a.c.n_kv_heads);
+  k_kv_plan<<<1, a.b.n_req <= 256 && p.cap <= 1024 ? 256 : NT_PLAN, psm, st>>>(a.b, p, a.c.n_kv_heads);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   if (D == 128) return half ? run<128, true>(a, p, m, st) : run<128, false>(a, p, m, st);
