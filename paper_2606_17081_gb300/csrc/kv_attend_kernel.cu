@@ -31,7 +31,7 @@ namespace {
 constexpr int TK = 128;        // keys of a tile
 // Costs: a tile of a job of at most 128 rows, one of a larger job, and a job's
 // own (its rows' loads and stores).
-constexpr int W_NARROW = 2, W_WIDE = 3, OV = 2;
+constexpr int W_NARROW = 4, W_WIDE = 6, OV_NARROW = 3, OV_WIDE = 10;
 constexpr int NT_PLAN = 1024;   // at most: 256 where that is a thread a request
 constexpr int NT_ATT = 384;
 constexpr int PLAN_GROUPS = 1024;   // groups whose sums are kept in shared memory
@@ -134,19 +134,23 @@ struct ReqLens {
 __device__ __forceinline__ int tiles(int keys) { return keys > 0 ? (keys + TK - 1) / TK : 0; }
 
 __device__ __forceinline__ int tile_cost(int flags) { return (flags & JOB_WIDE) ? W_WIDE : W_NARROW; }
+__device__ __forceinline__ int own_cost(int flags) { return (flags & JOB_WIDE) ? OV_WIDE : OV_NARROW; }
 // (a job without keys whose rows nobody else has writes their zeros)
 __device__ __forceinline__ int job_cost(int nt, int flags) {
-  return nt > 0 ? nt * tile_cost(flags) + OV : (flags & JOB_ALONE) ? OV : 0;
+  return nt > 0 ? nt * tile_cost(flags) + own_cost(flags) : (flags & JOB_ALONE) ? OV_NARROW : 0;
 }
 // The first tile that starts at cost `off` of a job or after it.
-__device__ __forceinline__ int tile_at(int off, int w) { return off <= OV ? 0 : (off - OV + w - 1) / w; }
+__device__ __forceinline__ int tile_at(int off, int flags) {
+  off -= own_cost(flags);
+  return off <= 0 ? 0 : (flags & JOB_WIDE) ? (off + W_WIDE - 1) / W_WIDE : (off + W_NARROW - 1) / W_NARROW;
+}
 
 // The tiles that CTA c has of a job and head of `cost` from u0 on.
-__device__ __forceinline__ bool segment(int64_t u0, int cost, int w, int nt, int64_t per, int64_t c, int& t0, int& t1) {
+__device__ __forceinline__ bool segment(int64_t u0, int cost, int flags, int nt, int64_t per, int64_t c, int& t0, int& t1) {
   const int64_t lo = max(c * per, u0) - u0, hi = min((c + 1) * per, u0 + cost) - u0;
   if (lo >= hi) return false;
-  t0 = min(tile_at((int)lo, w), nt);
-  t1 = min(tile_at((int)hi, w), nt);
+  t0 = min(tile_at((int)lo, flags), nt);
+  t1 = min(tile_at((int)hi, flags), nt);
   return t1 > t0;
 }
 
@@ -255,7 +259,7 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
       const int rt = t1 > t0 ? (t1 - t0 + w2 - 1) / w2 : 0;
       P = (int)min((unsigned long long)prefix_keys(g), of(4 * g + 3));   // (what nobody has written yet is not read)
       const unsigned long long with = of(4 * g + 1) + (unsigned long long)rt * job_cost(tiles(P), t1 - t0 > p.tpt ? JOB_WIDE : 0) +
-                                      (unsigned long long)(max(t1 - t0, 0) >> 1);
+                                      (unsigned long long)max(t1 - t0, 0);
       if (P > 0 && first < last && with < of(4 * g)) cnt = rt;
     }
     const int64_t at = jobs + block_scan(cnt, s_scan, &total);
@@ -350,7 +354,7 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
   __syncthreads();
   const int64_t all = cost * n_kv_heads;
   // two tiles at least, one for each stream of a CTA
-  const int64_t per = max((all + p.ctas - 1) / p.ctas, (int64_t)(2 * W_NARROW + OV));
+  const int64_t per = max((all + p.ctas - 1) / p.ctas, (int64_t)(2 * W_NARROW + OV_NARROW));
   __shared__ int s_cuts;
   if (tid == 0) s_cuts = 0;
   __syncthreads();
@@ -375,11 +379,10 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
       s.j = j;
       const int64_t u0 = u - s.off;
       if (s.off > 0 && j.nt > 0 && (j.flags & JOB_ALONE) && u0 >= u - per) {   // not cut before
-        const int w = tile_cost(j.flags);
         int t0, t1, e = (int)quotient(u0 + cj - 1, per);
         cut.c0 = c - 1;
-        cut.first = segment(u0, cj, w, j.nt, per, c - 1, t0, t1) ? c - 1 : c;
-        cut.last = segment(u0, cj, w, j.nt, per, e, t0, t1) ? e : e - 1;
+        cut.first = segment(u0, cj, j.flags, j.nt, per, c - 1, t0, t1) ? c - 1 : c;
+        cut.last = segment(u0, cj, j.flags, j.nt, per, e, t0, t1) ? e : e - 1;
         cut.tok0 = j.tok0;
         cut.head = s.head;
         cut.ntok = j.ntok;
@@ -634,10 +637,10 @@ struct Walk {
         ahead = jobs[++j];
         continue;
       }
-      const int take = (int)min((int64_t)(cost - off), rem), w = tile_cost(ahead.flags);
+      const int take = (int)min((int64_t)(cost - off), rem);
       const bool empty = ahead.nt == 0 && off == 0;
-      s.t0 = min(tile_at(off, w), ahead.nt);
-      s.t1 = min(tile_at(off + take, w), ahead.nt);
+      s.t0 = min(tile_at(off, ahead.flags), ahead.nt);
+      s.t1 = min(tile_at(off + take, ahead.flags), ahead.nt);
       s.cut_front = off > 0;
       s.head = h;
       s.job = ahead;
@@ -1196,13 +1199,13 @@ struct Parts {
 __device__ __forceinline__ Parts parts_of(const KvJob& j, int head, int n_kv_heads, const KvHead& hd) {
   Parts r{0, 0, 0, 0};
   if (j.nt <= 0) return r;
-  const int w = tile_cost(j.flags), cost = job_cost(j.nt, j.flags);
+  const int cost = job_cost(j.nt, j.flags);
   const int64_t u0 = j.cost * n_kv_heads + (int64_t)head * cost;
   const int64_t c0 = quotient(u0, hd.per), c1 = quotient(u0 + cost - 1, hd.per);
   int t0, t1;
   r.c0 = (int)c0;
-  r.first = (int)(segment(u0, cost, w, j.nt, hd.per, c0, t0, t1) ? c0 : c0 + 1);
-  r.last = (int)(segment(u0, cost, w, j.nt, hd.per, c1, t0, t1) ? c1 : c1 - 1);
+  r.first = (int)(segment(u0, cost, j.flags, j.nt, hd.per, c0, t0, t1) ? c0 : c0 + 1);
+  r.last = (int)(segment(u0, cost, j.flags, j.nt, hd.per, c1, t0, t1) ? c1 : c1 - 1);
   r.count = max(r.last - r.first + 1, 1);
   if (r.count == 1) r.last = r.first - 1;
   return r;
