@@ -35,7 +35,7 @@ constexpr int W_NARROW = 4, W_WIDE = 6, OV_NARROW = 3, OV_WIDE = 10;
 constexpr int NT_PLAN = 1024;   // at most: 256 where that is a thread a request
 constexpr int NT_ATT = 384;
 constexpr int PLAN_GROUPS = 1024;   // groups whose sums are kept in shared memory
-constexpr int PLAN_JOBS = 4096;     // jobs whose costs are
+constexpr int PLAN_JOBS = 1024;     // jobs that are
 
 constexpr int JOB_ALONE = 1;   // no other job has its rows
 constexpr int JOB_EVEN = 2;    // every row sees all the job's keys
@@ -103,27 +103,31 @@ __device__ __forceinline__ int clampi(int64_t x, int lo, int hi) {
   return (int)(x < lo ? lo : x > hi ? hi : x);
 }
 
-// Exclusive block sum of x; *total = the sum over the block.
-__device__ int64_t block_scan(int64_t x, int64_t* sm, int64_t* total) {
+struct JobSum {
+  int64_t count, cost;
+};
+
+// Exclusive block sum of x and its total; sm: one entry a warp, not the one of the
+// sum before.
+__device__ JobSum block_scan(JobSum x, JobSum* sm, JobSum& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int64_t s = x;
+  auto scan = [&](JobSum s) {
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int64_t y = __shfl_up_sync(~0u, s, o);
-    if (lane >= o) s += y;
-  }
-  __syncthreads();   // (sm may still be read from the scan before)
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t y = __shfl_up_sync(~0u, s.count, o);
+      const int64_t z = __shfl_up_sync(~0u, s.cost, o);
+      if (lane >= o) { s.count += y; s.cost += z; }
+    }
+    return s;
+  };
+  const JobSum s = scan(x);
   if (lane == 31) sm[warp] = s;
   __syncthreads();
-  int64_t w = lane < (blockDim.x >> 5) ? sm[lane] : 0, ws = w;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int64_t y = __shfl_up_sync(~0u, ws, o);
-    if (lane >= o) ws += y;
-  }
-  const int64_t before = __shfl_sync(~0u, ws - w, warp);
-  *total = __shfl_sync(~0u, ws, 31);
-  return before + s - x;
+  const JobSum w = lane < (int)(blockDim.x >> 5) ? sm[lane] : JobSum{0, 0}, ws = scan(w);
+  total.count = __shfl_sync(~0u, ws.count, 31);
+  total.cost = __shfl_sync(~0u, ws.cost, 31);
+  return JobSum{__shfl_sync(~0u, ws.count - w.count, warp) + s.count - x.count,
+                __shfl_sync(~0u, ws.cost - w.cost, warp) + s.cost - x.cost};
 }
 
 struct ReqLens {
@@ -161,17 +165,19 @@ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
 // One CTA: whether each group's prefix pays as one job for all its rows, the
 // jobs, their costs' sums, every CTA's start and what its end cuts.  Latency is
 // all that counts here (a few dependent reads and block sums): lengths are read
-// once at up to NT_PLAN requests, sums and costs live in shared memory at
-// ordinary sizes.
+// once at up to a request a thread, group sums and jobs live in shared memory at
+// ordinary sizes.  Starts that decrease can ask for more jobs than there is room
+// for: those get no work.
 __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, int n_kv_heads) {
-  extern __shared__ unsigned long long psm[];
-  int64_t* s_cost = reinterpret_cast<int64_t*>(psm);            // [PLAN_JOBS + 1]
-  unsigned long long* s_sum = psm + PLAN_JOBS + 1;               // [4 PLAN_GROUPS]
+  extern __shared__ __align__(16) unsigned char psm[];
+  KvJob* s_job = reinterpret_cast<KvJob*>(psm);                  // [PLAN_JOBS]
+  unsigned long long* s_sum = reinterpret_cast<unsigned long long*>(s_job + PLAN_JOBS);   // [4 PLAN_GROUPS]
   int32_t* s_start = reinterpret_cast<int32_t*>(s_sum + 4 * PLAN_GROUPS);   // [PLAN_GROUPS + 1]
   int32_t* s_prefix = s_start + PLAN_GROUPS + 1;                 // [PLAN_GROUPS]
   int32_t* s_gjob = s_prefix + PLAN_GROUPS;                      // [PLAN_GROUPS]
-  __shared__ int64_t s_scan[NT_PLAN / 32];
-  const int tid = threadIdx.x, nt = blockDim.x, n = b.n_req, G = b.n_groups;
+  __shared__ JobSum s_scan[2][NT_PLAN / 32];
+  __shared__ int s_cuts;
+  const int tid = threadIdx.x, lane = tid & 31, nth = blockDim.x, n = b.n_req, G = b.n_groups;
   const int w2 = 2 * p.tpt;
   const bool few = G <= PLAN_GROUPS;
   unsigned long long* sum = few ? s_sum : p.gsum;
@@ -202,23 +208,35 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
   ReqLens mine{0, 0, 0, -1};   // of request tid
   if (tid < n) mine = lens(tid);
   const int q_end = n > 0 ? rows_at(n) : 0;
-  if (few && G > 0) {
-    for (int g = tid; g <= G; g += nt) s_start[g] = b.group_start[g];
-    for (int g = tid; g < G; g += nt) s_prefix[g] = b.prefix_len[g];
+  if (tid == 0) s_cuts = 0;
+  JobSum jobs{0, 0}, total;
+  int turn = 0;
+  if (G > 0) {
+    if (few) {
+      for (int g = tid; g <= G; g += nth) s_start[g] = b.group_start[g];
+      for (int g = tid; g < G; g += nth) s_prefix[g] = b.prefix_len[g];
+    }
+    // of each group: its requests' costs without and with a shared prefix, whether
+    // some row sees less than the prefix, the longest context
+    for (int x = tid; x < 4 * G; x += nth) sum[x] = 0;
+    __syncthreads();
+    if (tid < n) mine.g = group(tid);
   }
-  // of each group: its requests' costs without and with a shared prefix, whether
-  // some row sees less than the prefix, the longest context
-  for (int x = tid; x < 4 * G; x += nt) sum[x] = 0;
-  __syncthreads();
-  mine.g = tid < n ? group(tid) : -1;
   auto request = [&](int i) {
     if (i == tid) return mine;
     ReqLens r = lens(i);
     r.g = group(i);
     return r;
   };
+  auto put = [&](JobSum at, KvJob j) {
+    if (at.count >= p.cap) return;
+    j.cost = at.cost;
+    j.reserved0 = 0;
+    p.jobs[at.count] = j;
+    if (at.count < PLAN_JOBS) s_job[at.count] = j;
+  };
   if (G > 0) {
-    for (int i = tid; i < n; i += nt) {
+    for (int i = tid; i < n; i += nth) {
       const ReqLens r = request(i);
       const int g = r.g;
       if (g < 0 || r.q == 0) continue;
@@ -229,7 +247,7 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
       const unsigned apart = __reduce_add_sync(peers, (unsigned)min((int64_t)rt * job_cost(tiles(seen), fl), (int64_t)top));
       const unsigned with = __reduce_add_sync(peers, (unsigned)min((int64_t)rt * job_cost(tiles(seen - P), fl), (int64_t)top));
       const unsigned less = __reduce_or_sync(peers, r.kv - r.q + 1 < P), most = __reduce_max_sync(peers, (unsigned)r.kv);
-      if ((tid & 31) == __ffs(peers) - 1) {
+      if (lane == __ffs(peers) - 1) {
         atomicAdd(&sum[4 * g], (unsigned long long)apart);
         atomicAdd(&sum[4 * g + 1], (unsigned long long)with);
         if (less) sum[4 * g + 2] = 1;
@@ -237,73 +255,66 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
       }
     }
     __syncthreads();
-  }
-  auto put = [&](int64_t at, const KvJob& j) {
-    if (at >= p.cap) return;
-    p.jobs[at] = j;
-    if (at < PLAN_JOBS) s_cost[at] = job_cost(j.nt, j.flags);
-  };
-  // prefix jobs.  Shared when that costs less: the group's prefix once for every
-  // w2 of its tokens, and a quarter of a tile a token for the parts' way
-  // through memory (2 parts written and read, 4 D bytes each a row, against
-  // 512 D bytes a tile).
-  int64_t jobs = 0, total;
-  for (int base = 0; base < G; base += nt) {
-    const int g = base + tid;
-    int cnt = 0, t0 = 0, t1 = 0, P = 0, first = 0;
-    if (g < G) {
-      first = clampi(gstart[g], 0, n);
-      const int last = clampi(gstart[g + 1], 0, n);
-      t0 = rows_at(first);
-      t1 = rows_at(max(first, last));
-      const int rt = t1 > t0 ? (t1 - t0 + w2 - 1) / w2 : 0;
-      P = (int)min((unsigned long long)prefix_keys(g), of(4 * g + 3));   // (what nobody has written yet is not read)
-      const unsigned long long with = of(4 * g + 1) + (unsigned long long)rt * job_cost(tiles(P), t1 - t0 > p.tpt ? JOB_WIDE : 0) +
-                                      (unsigned long long)max(t1 - t0, 0);
-      if (P > 0 && first < last && with < of(4 * g)) cnt = rt;
-    }
-    const int64_t at = jobs + block_scan(cnt, s_scan, &total);
-    jobs += total;
-    if (g < G) {
-      const bool fits = cnt > 0 && at + cnt <= p.cap;
-      gjob[g] = fits ? (int32_t)at : -1;
-      const bool even = of(4 * g + 2) == 0;
-      for (int k = 0; k < cnt; k++) {
+    // prefix jobs.  Shared when that costs less: the group's prefix once for every
+    // w2 of its tokens, and a quarter of a tile a token for the parts' way
+    // through memory (2 parts written and read, 4 D bytes each a row, against
+    // 512 D bytes a tile).
+    for (int base = 0; base < G; base += nth) {
+      const int g = base + tid;
+      int cnt = 0, t0 = 0, t1 = 0, P = 0, first = 0, last_flags = 0;
+      JobSum x{0, 0};
+      if (g < G) {
+        first = clampi(gstart[g], 0, n);
+        const int last = clampi(gstart[g + 1], 0, n);
+        t0 = rows_at(first);
+        t1 = rows_at(max(first, last));
+        const int rt = t1 > t0 ? (t1 - t0 + w2 - 1) / w2 : 0;
+        P = (int)min((unsigned long long)prefix_keys(g), of(4 * g + 3));   // (what nobody has written yet is not read)
+        last_flags = t1 - t0 - (rt - 1) * w2 > p.tpt ? JOB_WIDE : 0;
+        x.cost = (int64_t)(rt - 1) * job_cost(tiles(P), JOB_WIDE) + job_cost(tiles(P), last_flags);
+        if (P > 0 && first < last && rt > 0 && of(4 * g + 1) + x.cost + W_NARROW / 4 * (t1 - t0) < of(4 * g)) cnt = rt;
+        if (cnt == 0) x.cost = 0;
+        x.count = cnt;
+      }
+      JobSum at = block_scan(x, s_scan[turn ^= 1], total);
+      at.count += jobs.count;
+      at.cost += jobs.cost;
+      jobs.count += total.count;
+      jobs.cost += total.cost;
+      if (g < G) {
+        gjob[g] = cnt > 0 && at.count + cnt <= p.cap ? (int32_t)at.count : -1;
         KvJob j = {};
-        if (fits) {   // (else starts decrease: no work)
+        j.row = first;
+        j.kend = j.lim0 = P;
+        j.nt = tiles(P);
+        for (int k = 0; k < cnt; k++) {
           j.tok0 = t0 + k * w2;
           j.ntok = min(w2, t1 - j.tok0);
-          j.row = first;
-          j.kend = j.lim0 = P;
-          j.nt = tiles(P);
-          j.flags = JOB_PREFIX | (even ? JOB_EVEN : 0) | (j.ntok > p.tpt ? JOB_WIDE : 0);
+          j.flags = JOB_PREFIX | (of(4 * g + 2) == 0 ? JOB_EVEN : 0) | (k + 1 < cnt ? JOB_WIDE : last_flags);
+          put(at, j);
+          at.count++;
+          at.cost += job_cost(j.nt, j.flags);
         }
-        put(at + k, j);
       }
     }
+    __syncthreads();   // gjob
   }
-  jobs = min(jobs, (int64_t)p.cap);
-  const int prefix_jobs = (int)jobs;
-  __syncthreads();   // gjob
+  const int prefix_jobs = (int)min(jobs.count, (int64_t)p.cap);
   // the requests' own jobs
-  for (int base = 0; base < n; base += nt) {
+  for (int base = 0; base < n; base += nth) {
     const int i = base + tid;
     ReqLens r{0, 0, 0, -1};
-    int key0 = 0, cnt = 0;
-    bool alone = true;
+    int key0 = 0, alone = 1;
+    JobSum x{0, 0};
     if (i < n) {
       r = request(i);
       if (r.g >= 0 && gjob[r.g] >= 0) {
-        alone = false;
+        alone = 0;
         key0 = prefix_keys(r.g);
       }
-      cnt = (r.q + w2 - 1) / w2;
+      x.count = (r.q + w2 - 1) / w2;
     }
-    const int64_t at = jobs + block_scan(cnt, s_scan, &total);
-    jobs += total;
-    const bool fits = at + cnt <= p.cap;
-    if (i < n) p.job0[i] = cnt > 0 && fits ? (int32_t)at : -1;
-    auto job = [&](int k, int i, int q0, int q, int kv, int key0, bool alone) {
+    auto job = [&](int k, int i, int q0, int q, int kv, int key0, int alone) {
       KvJob j;
       const int a = k * w2, e = min(a + w2, q);
       j.tok0 = q0 + a;
@@ -317,59 +328,81 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
       return j;
     };
     // a request of one job is its thread's; a longer one is its warp's
-    if (cnt == 1) put(at, fits ? job(0, i, r.q0, r.q, r.kv, key0, alone) : KvJob{});
-    for (unsigned todo = __ballot_sync(~0u, cnt > 1); todo; todo &= todo - 1) {
+    const KvJob one = job(0, i, r.q0, r.q, r.kv, key0, alone);
+    if (x.count == 1) x.cost = job_cost(one.nt, one.flags);
+    const unsigned longer = __ballot_sync(~0u, x.count > 1);
+    for (unsigned todo = longer; todo; todo &= todo - 1) {
       const int src = __ffs(todo) - 1;
-      const int64_t sat = __shfl_sync(~0u, at, src);
-      const int sc = __shfl_sync(~0u, cnt, src), si = __shfl_sync(~0u, i, src);
-      const int s0 = __shfl_sync(~0u, r.q0, src), sq = __shfl_sync(~0u, r.q, src);
-      const int sk = __shfl_sync(~0u, r.kv, src), s1 = __shfl_sync(~0u, key0, src);
-      const bool sa = __shfl_sync(~0u, (int)alone, src), sf = __shfl_sync(~0u, (int)fits, src);
-      for (int k = tid & 31; k < sc; k += 32) put(sat + k, sf ? job(k, si, s0, sq, sk, s1, sa) : KvJob{});
+      const int sc = __shfl_sync(~0u, (int)x.count, src), sq = __shfl_sync(~0u, r.q, src), sk = __shfl_sync(~0u, r.kv, src);
+      const int s1 = __shfl_sync(~0u, key0, src), sa = __shfl_sync(~0u, alone, src);
+      int64_t c = 0;
+      for (int k = lane; k < sc; k += 32) {
+        const KvJob j = job(k, 0, 0, sq, sk, s1, sa);
+        c += job_cost(j.nt, j.flags);
+      }
+#pragma unroll
+      for (int o = 16; o; o >>= 1) c += __shfl_xor_sync(~0u, c, o);
+      if (lane == src) x.cost = c;
+    }
+    JobSum at = block_scan(x, s_scan[turn ^= 1], total);
+    at.count += jobs.count;
+    at.cost += jobs.cost;
+    jobs.count += total.count;
+    jobs.cost += total.cost;
+    if (i < n) p.job0[i] = x.count > 0 && at.count + x.count <= p.cap ? (int32_t)at.count : -1;
+    if (x.count == 1) put(at, one);
+    for (unsigned todo = longer; todo; todo &= todo - 1) {
+      const int src = __ffs(todo) - 1;
+      const int sc = __shfl_sync(~0u, (int)x.count, src), si = __shfl_sync(~0u, i, src);
+      const int s0 = __shfl_sync(~0u, r.q0, src), sq = __shfl_sync(~0u, r.q, src), sk = __shfl_sync(~0u, r.kv, src);
+      const int s1 = __shfl_sync(~0u, key0, src), sa = __shfl_sync(~0u, alone, src);
+      JobSum sat{__shfl_sync(~0u, at.count, src), __shfl_sync(~0u, at.cost, src)};
+      for (int k0 = 0; k0 < sc; k0 += 32) {
+        const int k = k0 + lane;
+        const KvJob j = job(min(k, sc - 1), si, s0, sq, sk, s1, sa);
+        const int64_t c = k < sc ? job_cost(j.nt, j.flags) : 0;
+        int64_t before = c;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int64_t y = __shfl_up_sync(~0u, before, o);
+          if (lane >= o) before += y;
+        }
+        if (k < sc) put(JobSum{sat.count + k, sat.cost + before - c}, j);
+        sat.cost += __shfl_sync(~0u, before, 31);
+      }
     }
   }
   // rows of no request: jobs without keys
   const int pads = (b.n_tokens - q_end + w2 - 1) / w2;
-  for (int k = tid; k < pads; k += nt) {
+  for (int k = tid; k < pads; k += nth) {
     KvJob j = {};
     j.tok0 = q_end + k * w2;
     j.ntok = min(w2, b.n_tokens - j.tok0);
     j.flags = JOB_ALONE | (j.ntok > p.tpt ? JOB_WIDE : 0);
-    put(jobs + k, j);
+    put(JobSum{jobs.count + k, jobs.cost + (int64_t)k * OV_NARROW}, j);
   }
-  const int J = (int)min(jobs + pads, (int64_t)p.cap);
   __syncthreads();   // the jobs
-  int64_t cost = 0;
-  for (int base = 0; base < J; base += nt) {
-    const int j = base + tid;
-    int64_t c = 0;
-    if (j < J) c = j < PLAN_JOBS ? s_cost[j] : job_cost(p.jobs[j].nt, p.jobs[j].flags);
-    const int64_t at = cost + block_scan(c, s_scan, &total);
-    cost += total;
-    if (j < J) {
-      p.jobs[j].cost = at;
-      if (j < PLAN_JOBS) s_cost[j] = at;
-    }
+  // (with more jobs than room the rest has no work: the last one's end is the total)
+  const int J = (int)min(jobs.count + pads, (int64_t)p.cap);
+  auto job_at = [&](int j) { return j < PLAN_JOBS ? s_job[j] : p.jobs[j]; };
+  auto cost_at = [&](int j) { return j < PLAN_JOBS ? s_job[j].cost : p.jobs[j].cost; };
+  int64_t all = 0;
+  if (J > 0) {
+    const KvJob j = job_at(J - 1);
+    all = (j.cost + job_cost(j.nt, j.flags)) * n_kv_heads;
   }
-  __syncthreads();
-  const int64_t all = cost * n_kv_heads;
   // two tiles at least, one for each stream of a CTA
   const int64_t per = max((all + p.ctas - 1) / p.ctas, (int64_t)(2 * W_NARROW + OV_NARROW));
-  __shared__ int s_cuts;
-  if (tid == 0) s_cuts = 0;
-  __syncthreads();
-  for (int c = tid; c < p.ctas; c += nt) {
+  for (int c = tid; c < p.ctas; c += nth) {
     const int64_t u = c * per;
     KvStart s = {};
-    KvCut cut = {};
     if (u < all) {
       int lo = 0, hi = J;   // the last job that starts at or before u
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        const int64_t at = mid < PLAN_JOBS ? s_cost[mid] : p.jobs[mid].cost;
-        if (at * n_kv_heads <= u) lo = mid; else hi = mid;
+        if (cost_at(mid) * n_kv_heads <= u) lo = mid; else hi = mid;
       }
-      const KvJob j = p.jobs[lo];
+      const KvJob j = job_at(lo);
       const int cj = job_cost(j.nt, j.flags);
       const int64_t in = u - j.cost * n_kv_heads;
       s.job = lo;
@@ -380,6 +413,7 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
       const int64_t u0 = u - s.off;
       if (s.off > 0 && j.nt > 0 && (j.flags & JOB_ALONE) && u0 >= u - per) {   // not cut before
         int t0, t1, e = (int)quotient(u0 + cj - 1, per);
+        KvCut cut = {};
         cut.c0 = c - 1;
         cut.first = segment(u0, cj, j.flags, j.nt, per, c - 1, t0, t1) ? c - 1 : c;
         cut.last = segment(u0, cj, j.flags, j.nt, per, e, t0, t1) ? e : e - 1;
@@ -1470,10 +1504,10 @@ cudaError_t launch_kv_attend(const KvAttendArgs& a, void* ws, int32_t* err, int 
   if (!encode(&m[0], half, a.c.k, 4, ks, kst, kbox) || !encode(&m[1], half, a.c.v, 4, ks, kst, kbox) ||
       !encode(&m[2], half, a.q, 3, qs, qst, qbox) || !encode(&m[3], half, a.q, 3, qs, qst, qbox1))
     return cudaErrorInvalidValue;
-  const size_t psm = (size_t)(PLAN_JOBS + 1 + 4 * PLAN_GROUPS) * 8 + (size_t)(3 * PLAN_GROUPS + 1) * 4;
+  const size_t psm = PLAN_JOBS * sizeof(KvJob) + (size_t)4 * PLAN_GROUPS * 8 + (size_t)(3 * PLAN_GROUPS + 1) * 4;
   cudaError_t e = cudaFuncSetAttribute(k_kv_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)psm);
   if (e != cudaSuccess) return e;
-  k_kv_plan<<<1, a.b.n_req <= 256 && p.cap <= 1024 ? 256 : NT_PLAN, psm, st>>>(a.b, p, a.c.n_kv_heads);
+  k_kv_plan<<<1, a.b.n_req <= 256 && a.b.n_groups <= 256 && p.cap <= PLAN_JOBS ? 256 : NT_PLAN, psm, st>>>(a.b, p, a.c.n_kv_heads);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   if (D == 128) return half ? run<128, true>(a, p, m, st) : run<128, false>(a, p, m, st);

@@ -317,10 +317,14 @@ def _refuse(what: str):
     raise RoutesimError(RS_ERR_INVALID, what)
 
 
-def _is_dev(x, dtype, what: str, dims: int = 1):
-    """The C entry points see pointers only: type, place and shape are checked here."""
-    if not x.is_cuda or x.dtype != dtype or x.dim() != dims or (dims and x.stride(-1) != 1 and x.size(-1) > 1):
-        _refuse(f"{what} must be a {dims}-dimensional {dtype} tensor on the GPU with unit last stride")
+# The C entry points see pointers only: types, places and shapes are checked here.  A step calls
+# these once a layer, so they take attributes once and avoid calls of their own.
+
+def _vector(x, dtype, n: int, what: str) -> int:
+    """Address of a tensor of n entries on the GPU."""
+    if x.dtype is not dtype or not x.is_cuda or x.dim() != 1 or x.numel() != n or (n > 1 and x.stride(0) != 1):
+        _refuse(f"{what} must be a contiguous {dtype} tensor of {n} entries on the GPU")
+    return x.data_ptr()
 
 
 class KVCache:
@@ -332,13 +336,14 @@ class KVCache:
     def __init__(self, k, v):
         import torch
         types = {torch.bfloat16: RS_BF16, torch.float16: RS_FP16}
-        if k.dtype not in types:
+        if k.dtype not in types or v.dtype != k.dtype:
             _refuse("the cache must be bfloat16 or float16")
-        _is_dev(k, k.dtype, "k", 4)
-        _is_dev(v, k.dtype, "v", 4)
+        if not k.is_cuda or not v.is_cuda or k.dim() != 4 or k.stride(3) != 1:
+            _refuse("k and v must be on the GPU, [block, kv head, 16, head_dim] with unit last stride")
         if k.shape != v.shape or k.stride() != v.stride() or k.shape[2] != 16:
             _refuse("k and v must have one shape [block, kv head, 16, head_dim] and one set of strides")
         self.k, self.v = k, v
+        self.dtype, self.kv_heads, self.head_dim = k.dtype, k.shape[1], k.shape[3]
         self.desc = rs_kv_cache(k.data_ptr(), v.data_ptr(), types[k.dtype], k.shape[1], k.shape[3], 0,
                                 k.shape[0], k.stride(0), k.stride(1), k.stride(2))
         self.ref = C.byref(self.desc)
@@ -352,28 +357,24 @@ class KVBatch:
 
     def __init__(self, table, q_start, kv_len, n_tokens: int, group_start=None, prefix_len=None):
         import torch
-        _is_dev(table, torch.int32, "table", 2)
-        _is_dev(q_start, torch.int32, "q_start")
-        _is_dev(kv_len, torch.int32, "kv_len")
+        self.int32, self.int64 = torch.int32, torch.int64
+        if table.dtype != torch.int32 or not table.is_cuda or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
+            _refuse("table must be an int32 matrix on the GPU with contiguous rows")
         n = table.shape[0]
-        groups = 0
+        starts = _vector(q_start, torch.int32, n + 1, "q_start")
+        lens = _vector(kv_len, torch.int32, n, "kv_len")
+        groups, first, prefix = 0, None, None
         if group_start is not None or prefix_len is not None:
             if group_start is None or prefix_len is None:
                 _refuse("group_start and prefix_len go together")
-            _is_dev(group_start, torch.int32, "group_start")
-            _is_dev(prefix_len, torch.int32, "prefix_len")
             groups = prefix_len.numel()
-            if group_start.numel() != groups + 1:
-                _refuse("group_start has one entry more than prefix_len")
-        if q_start.numel() != n + 1 or kv_len.numel() != n:
-            _refuse("q_start has n_req + 1 entries and kv_len n_req")
+            prefix = _vector(prefix_len, torch.int32, groups, "prefix_len")
+            first = _vector(group_start, torch.int32, groups + 1, "group_start")
         self.tensors = (table, q_start, kv_len, group_start, prefix_len)
-        self.n_tokens = n_tokens
+        self.n_req, self.n_tokens, self.n_groups = n, n_tokens, groups
         self.desc = rs_kv_batch(n, n_tokens, groups, table.shape[1],
                                 table.stride(0) if n > 1 else table.shape[1], table.data_ptr(),
-                                q_start.data_ptr(), kv_len.data_ptr(),
-                                group_start.data_ptr() if groups else None,
-                                prefix_len.data_ptr() if groups else None)
+                                starts, lens, first if groups else None, prefix if groups else None)
         self.ref = C.byref(self.desc)
 
 
@@ -382,63 +383,53 @@ def kv_tables(ctx, batch: KVBatch, q_len, prev_len, prefix_blocks, free, positio
     """Fills batch's table, q_start and kv_len, and positions int32 [n_tokens],
     slots int64 [n_tokens], counts int64 [2] (blocks needed, tokens).
     prefix_blocks: int32 [n_groups, longest prefix in blocks] or None; free: int32."""
-    import torch
-    n = batch.desc.n_req
-    for x, what in ((q_len, "q_len"), (prev_len, "prev_len")):
-        _is_dev(x, torch.int32, what)
-        if x.numel() != n:
-            _refuse(f"{what} has n_req entries")
-    _is_dev(free, torch.int32, "free")
-    _is_dev(positions, torch.int32, "positions")
-    _is_dev(slots, torch.int64, "slots")
-    _is_dev(counts, torch.int64, "counts")
-    if positions.numel() != batch.n_tokens or slots.numel() != batch.n_tokens or counts.numel() != 2:
-        _refuse("positions and slots have n_tokens entries, counts 2")
+    n, rows, i32, i64 = batch.n_req, batch.n_tokens, batch.int32, batch.int64
     pb, ps = None, 0
-    if batch.desc.n_groups:
-        _is_dev(prefix_blocks, torch.int32, "prefix_blocks", 2)
-        if prefix_blocks.shape[0] != batch.desc.n_groups:
-            _refuse("prefix_blocks has a row a group")
+    if batch.n_groups:
+        if prefix_blocks is None or prefix_blocks.dtype is not i32 or not prefix_blocks.is_cuda or prefix_blocks.dim() != 2 \
+                or prefix_blocks.shape[0] != batch.n_groups or not prefix_blocks.is_contiguous():
+            _refuse("prefix_blocks must be a contiguous int32 matrix on the GPU with a row a group")
         pb, ps = prefix_blocks.data_ptr(), prefix_blocks.shape[1]
-        if prefix_blocks.shape[0] > 1 and prefix_blocks.stride(0) != ps:
-            _refuse("prefix_blocks must be contiguous")
-    st = lib().kv_tables(ctx, batch.ref, q_len.data_ptr(), prev_len.data_ptr(), pb, ps,
-                         free.data_ptr(), free.numel(), positions.data_ptr(), slots.data_ptr(),
-                         counts.data_ptr())
-    if st != RS_OK:
+    n_free = free.numel()
+    st = (_lib or lib()).kv_tables(
+        ctx, batch.ref, _vector(q_len, i32, n, "q_len"), _vector(prev_len, i32, n, "prev_len"), pb, ps,
+        _vector(free, i32, n_free, "free"), n_free, _vector(positions, i32, rows, "positions"),
+        _vector(slots, i64, rows, "slots"), _vector(counts, i64, 2, "counts"))
+    if st:
         _check(st, ctx)
 
 
 def kv_append(ctx, cache: KVCache, k, v, slots) -> None:
     """k, v [n_tokens, kv heads, head_dim] into the cache at slots int64 [n_tokens]."""
     import torch
-    d = cache.desc
-    _is_dev(k, cache.k.dtype, "k", 3)
-    _is_dev(v, cache.k.dtype, "v", 3)
-    _is_dev(slots, torch.int64, "slots")
-    if k.shape != v.shape or k.stride() != v.stride() or tuple(k.shape) != (slots.numel(), d.n_kv_heads, d.head_dim):
-        _refuse("k and v must be [n_tokens, kv heads, head_dim] of one set of strides, slots [n_tokens]")
-    st = lib().kv_append(ctx, cache.ref, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
-                         k.shape[0], slots.data_ptr())
-    if st != RS_OK:
+    n = slots.numel()
+    shape, stride, dtype = k.shape, k.stride(), cache.dtype
+    if k.dtype is not dtype or v.dtype is not dtype or not k.is_cuda or not v.is_cuda or v.shape != shape or v.stride() != stride:
+        _refuse("k and v must be on the GPU, of the cache's type, one shape and one set of strides")
+    if len(shape) != 3 or shape[0] != n or shape[1] != cache.kv_heads or shape[2] != cache.head_dim or stride[2] != 1:
+        _refuse("k and v must be [n_tokens, kv heads, head_dim] with unit last stride, slots [n_tokens]")
+    st = (_lib or lib()).kv_append(ctx, cache.ref, k.data_ptr(), v.data_ptr(), stride[0], stride[1], n,
+                                   _vector(slots, torch.int64, n, "slots"))
+    if st:
         _check(st, ctx)
 
 
 def kv_attend(ctx, cache: KVCache, batch: KVBatch, q, scale: float, out, lse=None) -> None:
     """q, out [n_tokens, heads, head_dim] of the cache's type; lse float32 [n_tokens, heads] or None."""
-    import torch
-    _is_dev(q, cache.k.dtype, "q", 3)
-    _is_dev(out, cache.k.dtype, "out", 3)
-    if q.shape != out.shape or q.shape[0] != batch.n_tokens or q.shape[2] != cache.desc.head_dim:
-        _refuse("q and out must be [n_tokens, heads, head_dim]")
+    shape, qs, os, dtype = q.shape, q.stride(), out.stride(), cache.dtype
+    if q.dtype is not dtype or out.dtype is not dtype or not q.is_cuda or not out.is_cuda or out.shape != shape:
+        _refuse("q and out must be on the GPU, of the cache's type and one shape")
+    if len(shape) != 3 or shape[0] != batch.n_tokens or shape[2] != cache.head_dim or qs[2] != 1 or os[2] != 1:
+        _refuse("q and out must be [n_tokens, heads, head_dim] with unit last stride")
+    lp = None
     if lse is not None:
-        _is_dev(lse, torch.float32, "lse", 2)
-        if lse.shape != q.shape[:2] or not lse.is_contiguous():
-            _refuse("lse must be a contiguous [n_tokens, heads]")
-    st = lib().kv_attend(ctx, cache.ref, batch.ref, q.data_ptr(), q.shape[1], q.stride(0), q.stride(1),
-                         scale, out.data_ptr(), out.stride(0), out.stride(1),
-                         lse.data_ptr() if lse is not None else None)
-    if st != RS_OK:
+        if not lse.is_cuda or not lse.is_contiguous() or lse.element_size() != 4 or not lse.is_floating_point() \
+                or lse.dim() != 2 or lse.shape[0] != shape[0] or lse.shape[1] != shape[1]:
+            _refuse("lse must be a contiguous float32 [n_tokens, heads] on the GPU")
+        lp = lse.data_ptr()
+    st = (_lib or lib()).kv_attend(ctx, cache.ref, batch.ref, q.data_ptr(), shape[1], qs[0], qs[1], scale,
+                                   out.data_ptr(), os[0], os[1], lp)
+    if st:
         _check(st, ctx)
 
 
