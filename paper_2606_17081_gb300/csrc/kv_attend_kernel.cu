@@ -32,7 +32,7 @@ constexpr int TK = 128;        // keys of a tile
 // Costs: a tile of a job of at most 128 rows, one of a larger job, and a job's
 // own (its rows' loads and stores).
 constexpr int W_NARROW = 4, W_WIDE = 6, OV_NARROW = 3, OV_WIDE = 10;
-constexpr int NT_PLAN = 1024;   // at most: 256 where that is a thread a request
+constexpr int NT_PLAN = 1024;
 constexpr int NT_ATT = 384;
 constexpr int PLAN_GROUPS = 1024;   // groups whose sums are kept in shared memory
 constexpr int PLAN_JOBS = 1024;     // jobs that are
@@ -77,6 +77,7 @@ struct __align__(16) KvStart {
 };
 
 struct KvPlan {
+  unsigned* meet;       // [2] CTAs that have arrived, times that all have; 0 at first
   KvHead* head;
   KvJob* jobs;          // [cap + 1]
   int32_t* job0;        // [n_req] first own job, or -1
@@ -93,6 +94,8 @@ struct KvPlan {
   int32_t ctas;
   int32_t tpt;          // tokens of 128 rows
   int32_t ratio;        // heads of a kv head
+  int32_t planned;      // the plan is there before the attention kernel begins
+  int32_t join_here;    // the attention kernel joins the parts itself
 };
 
 namespace {
@@ -162,21 +165,31 @@ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
   return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
 }
 
-// One CTA: whether each group's prefix pays as one job for all its rows, the
-// jobs, their costs' sums, every CTA's start and what its end cuts.  Latency is
+// A plan's working memory.
+struct PlanSmem {
+  KvJob job[PLAN_JOBS];
+  unsigned long long sum[4 * PLAN_GROUPS];
+  int32_t start[PLAN_GROUPS + 1], prefix[PLAN_GROUPS], gjob[PLAN_GROUPS];
+  JobSum scan[2][32];
+  int32_t cuts;
+};
+
+// By a whole CTA: whether each group's prefix pays as one job for all its rows,
+// the jobs, their costs' sums, every CTA's start and what its end cuts.  Latency is
 // all that counts here (a few dependent reads and block sums): lengths are read
 // once at up to a request a thread, group sums and jobs live in shared memory at
 // ordinary sizes.  Starts that decrease can ask for more jobs than there is room
 // for: those get no work.
-__global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, int n_kv_heads) {
-  extern __shared__ __align__(16) unsigned char psm[];
-  KvJob* s_job = reinterpret_cast<KvJob*>(psm);                  // [PLAN_JOBS]
-  unsigned long long* s_sum = reinterpret_cast<unsigned long long*>(s_job + PLAN_JOBS);   // [4 PLAN_GROUPS]
-  int32_t* s_start = reinterpret_cast<int32_t*>(s_sum + 4 * PLAN_GROUPS);   // [PLAN_GROUPS + 1]
-  int32_t* s_prefix = s_start + PLAN_GROUPS + 1;                 // [PLAN_GROUPS]
-  int32_t* s_gjob = s_prefix + PLAN_GROUPS;                      // [PLAN_GROUPS]
-  __shared__ JobSum s_scan[2][NT_PLAN / 32];
-  __shared__ int s_cuts;
+//   all = true: one CTA for everybody, starts into p.start.
+//   all = false (at most PLAN_JOBS jobs and PLAN_GROUPS groups): every CTA for
+//     itself, its start into *mine and the jobs of its share into p.jobs; what the
+//     joining needs is written by CTA 0.
+__device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p, int n_kv_heads, PlanSmem& ps, bool all_ctas,
+                                          KvStart* own_start, KvHead* own_head) {
+  const bool writer = all_ctas || blockIdx.x == 0;
+  KvJob* s_job = ps.job;
+  unsigned long long* s_sum = ps.sum;
+  int32_t *s_start = ps.start, *s_prefix = ps.prefix, *s_gjob = ps.gjob;
   const int tid = threadIdx.x, lane = tid & 31, nth = blockDim.x, n = b.n_req, G = b.n_groups;
   const int w2 = 2 * p.tpt;
   const bool few = G <= PLAN_GROUPS;
@@ -184,7 +197,6 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
   const int32_t* gstart = few ? s_start : b.group_start;
   const int32_t* glen = few ? s_prefix : b.prefix_len;
   int32_t* gjob = few ? s_gjob : p.gjob;
-  asm volatile("griddepcontrol.launch_dependents;");
 
   auto of = [&](int x) { return few ? s_sum[x] : __ldcg(p.gsum + x); };
   auto prefix_keys = [&](int g) { return (int)min((int64_t)(max(glen[g], 0) & ~15), (int64_t)b.max_blocks * 16); };
@@ -208,7 +220,7 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
   ReqLens mine{0, 0, 0, -1};   // of request tid
   if (tid < n) mine = lens(tid);
   const int q_end = n > 0 ? rows_at(n) : 0;
-  if (tid == 0) s_cuts = 0;
+  if (tid == 0) ps.cuts = 0;
   JobSum jobs{0, 0}, total;
   int turn = 0;
   if (G > 0) {
@@ -232,7 +244,7 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
     if (at.count >= p.cap) return;
     j.cost = at.cost;
     j.reserved0 = 0;
-    p.jobs[at.count] = j;
+    if (writer) p.jobs[at.count] = j;
     if (at.count < PLAN_JOBS) s_job[at.count] = j;
   };
   if (G > 0) {
@@ -276,7 +288,7 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
         if (cnt == 0) x.cost = 0;
         x.count = cnt;
       }
-      JobSum at = block_scan(x, s_scan[turn ^= 1], total);
+      JobSum at = block_scan(x, ps.scan[turn ^= 1], total);
       at.count += jobs.count;
       at.cost += jobs.cost;
       jobs.count += total.count;
@@ -344,12 +356,12 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
       for (int o = 16; o; o >>= 1) c += __shfl_xor_sync(~0u, c, o);
       if (lane == src) x.cost = c;
     }
-    JobSum at = block_scan(x, s_scan[turn ^= 1], total);
+    JobSum at = block_scan(x, ps.scan[turn ^= 1], total);
     at.count += jobs.count;
     at.cost += jobs.cost;
     jobs.count += total.count;
     jobs.cost += total.cost;
-    if (i < n) p.job0[i] = x.count > 0 && at.count + x.count <= p.cap ? (int32_t)at.count : -1;
+    if (writer && i < n) p.job0[i] = x.count > 0 && at.count + x.count <= p.cap ? (int32_t)at.count : -1;
     if (x.count == 1) put(at, one);
     for (unsigned todo = longer; todo; todo &= todo - 1) {
       const int src = __ffs(todo) - 1;
@@ -420,13 +432,34 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, in
         cut.tok0 = j.tok0;
         cut.head = s.head;
         cut.ntok = j.ntok;
-        if (cut.first < cut.last) p.cut[atomicAdd(&s_cuts, 1)] = cut;   // (else whole in one CTA)
+        if (cut.first < cut.last) {   // (else whole in one CTA)
+          const int at = atomicAdd(&ps.cuts, 1);
+          if (writer) p.cut[at] = cut;
+        }
       }
     }
-    p.start[c] = s;
+    if (all_ctas) p.start[c] = s;
+    else if (c == (int)blockIdx.x) *own_start = s;
+  }
+  if (!all_ctas) {
+    const int64_t u = blockIdx.x * per;
+    for (int j = tid; j < J; j += nth) {
+      const KvJob x = s_job[j];
+      const int64_t at = x.cost * n_kv_heads;
+      if (at < u + per && at + (int64_t)job_cost(x.nt, x.flags) * n_kv_heads > u) p.jobs[j] = x;
+    }
   }
   __syncthreads();
-  if (tid == 0) *p.head = KvHead{all, per, J, prefix_jobs, s_cuts, 0};
+  if (tid == 0) {
+    const KvHead h{all, per, J, prefix_jobs, ps.cuts, 0};
+    if (writer) *p.head = h;
+    if (!all_ctas) *own_head = h;
+  }
+}
+
+__global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, int n_kv_heads) {
+  extern __shared__ __align__(16) unsigned char psm[];
+  make_plan(b, p, n_kv_heads, *reinterpret_cast<PlanSmem*>(psm), true, nullptr, nullptr);
 }
 
 // ------------------------------------------------------------------ PTX
@@ -618,6 +651,165 @@ __device__ __forceinline__ void row_exp(float sl, float nm, uint32_t* v, float& 
 
 __device__ __forceinline__ float minus(float m, float sl) { return m == -INFINITY ? 0.0f : -__fmul_rn(m, sl); }
 
+// ------------------------------------------------------------------ joining
+
+// Where the parts of a job and head are: whole in its place among all rows (one
+// part, last < first), or in CTAs first .. last.
+struct Parts {
+  int c0, first, last, count;
+};
+
+__device__ __forceinline__ Parts parts_of(const KvJob& j, int head, int n_kv_heads, const KvHead& hd) {
+  Parts r{0, 0, 0, 0};
+  if (j.nt <= 0) return r;
+  const int cost = job_cost(j.nt, j.flags);
+  const int64_t u0 = j.cost * n_kv_heads + (int64_t)head * cost;
+  const int64_t c0 = quotient(u0, hd.per), c1 = quotient(u0 + cost - 1, hd.per);
+  int t0, t1;
+  r.c0 = (int)c0;
+  r.first = (int)(segment(u0, cost, j.flags, j.nt, hd.per, c0, t0, t1) ? c0 : c0 + 1);
+  r.last = (int)(segment(u0, cost, j.flags, j.nt, hd.per, c1, t0, t1) ? c1 : c1 - 1);
+  r.count = max(r.last - r.first + 1, 1);
+  if (r.count == 1) r.last = r.first - 1;
+  return r;
+}
+
+__device__ __forceinline__ KvJob job_from_l2(const KvJob* j) {
+  KvJob r;
+  const int4* s = reinterpret_cast<const int4*>(j);
+  int4* d = reinterpret_cast<int4*>(&r);
+#pragma unroll
+  for (int k = 0; k < 3; k++) d[k] = __ldcg(s + k);
+  return r;
+}
+
+// One row (token, head) from its parts: x's (row rx of the 256 if cut, else at
+// home), then y's.  A lane takes the log sum of a part, the warp their largest
+// and the weights, and the rows of several parts are on their way at once.
+template <int D, bool HALF>
+__device__ __forceinline__ void join_row(const KvAttendArgs& a, const KvPlan& p, const Parts& x, int rx, const Parts& y, int ry,
+                                         int64_t row, int hq, int lane) {
+  constexpr int E = D / 32;
+  const int64_t home = row * a.n_heads + hq, all = (int64_t)a.b.n_tokens * a.n_heads;
+  const int count = x.count + y.count;
+  float m = -INFINITY, l = 0.0f, o[E];
+#pragma unroll
+  for (int e = 0; e < E; e++) o[e] = 0.0f;
+  for (int base = 0; base < count; base += 32) {
+    const int k = base + lane;
+    const float* src = nullptr;
+    float s = -INFINITY;
+    if (k < count) {
+      const Parts& q = k < x.count ? x : y;
+      const int c = q.first + (k < x.count ? k : k - x.count);
+      const bool whole = q.last < q.first;
+      const int64_t at = whole ? (k < x.count ? 0 : all) + home
+                               : ((int64_t)c * 2 + (c == q.c0 ? 1 : 0)) * 256 + (k < x.count ? rx : ry);
+      s = __ldcg((whole ? p.home_lse : p.part_lse) + at);
+      src = (whole ? p.home : p.part) + at * D;
+    }
+    float big = s;
+#pragma unroll
+    for (int z = 16; z; z >>= 1) big = fmaxf(big, __shfl_xor_sync(~0u, big, z));
+    const float m2 = fmaxf(m, big);
+    const float wt = s == -INFINITY ? 0.0f : ex2(__fsub_rn(s, m2));
+    const float f = m == -INFINITY ? 0.0f : ex2(__fsub_rn(m, m2));
+    float sum = wt;
+#pragma unroll
+    for (int z = 16; z; z >>= 1) sum = __fadd_rn(sum, __shfl_xor_sync(~0u, sum, z));
+    l = fmaf(l, f, sum);
+#pragma unroll
+    for (int e = 0; e < E; e++) o[e] = __fmul_rn(o[e], f);
+    m = m2;
+    const int here = min(32, count - base);
+    for (int q = 0; q < here; q += 8) {
+      float w8[8], v[8][E];
+#pragma unroll
+      for (int z = 0; z < 8; z++) {   // (past the last part: weight 0, the last one's row)
+        const int from = min(q + z, here - 1);
+        const float w = __shfl_sync(~0u, wt, from);
+        w8[z] = q + z < here ? w : 0.0f;
+        const float* r = reinterpret_cast<const float*>(__shfl_sync(~0u, reinterpret_cast<unsigned long long>(src), from)) + lane * E;
+        if constexpr (E == 4) {
+          const float4 t = __ldcg(reinterpret_cast<const float4*>(r));
+          v[z][0] = t.x; v[z][1] = t.y; v[z][2] = t.z; v[z][3] = t.w;
+        } else {
+          const float2 t = __ldcg(reinterpret_cast<const float2*>(r));
+          v[z][0] = t.x; v[z][1] = t.y;
+        }
+      }
+#pragma unroll
+      for (int z = 0; z < 8; z++)
+#pragma unroll
+        for (int e = 0; e < E; e++) o[e] = w8[z] == 0.0f ? o[e] : fmaf(w8[z], v[z][e], o[e]);
+    }
+  }
+  const float inv = l == 0.0f ? 0.0f : __fdiv_rn(1.0f, l);
+  uint16_t* out = static_cast<uint16_t*>(a.out) + row * a.o_ts + hq * a.o_hs + lane * E;
+  uint32_t z[E / 2];
+#pragma unroll
+  for (int e = 0; e < E; e += 2) z[e / 2] = pack2<HALF>(__fmul_rn(o[e], inv), __fmul_rn(o[e + 1], inv));
+  if constexpr (E == 4) *reinterpret_cast<uint2*>(out) = make_uint2(z[0], z[1]);
+  else *reinterpret_cast<uint32_t*>(out) = z[0];
+  if (a.lse && lane == 0)
+    a.lse[home] = l == 0.0f ? -INFINITY : __fmul_rn(__fadd_rn(m, __log2f(l)), 0.6931471805599453f);
+}
+
+// Rows that have parts, a warp a row: of the jobs that a share's end cut, and of
+// shared groups, whose rows have a prefix job and an own one.  The parts' order
+// is the keys', so the result does not depend on when they came.
+template <int D, bool HALF>
+__device__ __forceinline__ void join_rows(const KvAttendArgs& a, const KvPlan& p, const KvHead& hd, int first, int step) {
+  const int lane = threadIdx.x & 31;
+  const int hk = a.c.n_kv_heads, w2 = 2 * p.tpt, n = a.b.n_req;
+  const int64_t cuts = (int64_t)hd.cuts * 256, rows = cuts + (int64_t)hd.prefix_jobs * hk * 256;
+  for (int64_t x = first; x < rows; x += step) {
+    const int rr = (int)(x & 255), r = rr & 127, tl = r / p.ratio, hl = r - tl * p.ratio;   // of a job's 256
+    const int tok = (rr >> 7) * p.tpt + tl;
+    Parts pre{0, 0, 0, 0}, own{0, 0, 0, 0};
+    int row, hq, ro = 0;
+    if (x < cuts) {
+      const int4* c = reinterpret_cast<const int4*>(p.cut + (x >> 8));
+      const int4 c0 = __ldcg(c), c1 = __ldcg(c + 1);
+      if (tl >= p.tpt || tok >= c0.y) continue;
+      pre = Parts{c0.w, c1.x, c1.y, c1.y - c1.x + 1};
+      row = c0.x + tok;
+      hq = c0.z * p.ratio + hl;
+    } else {
+      const int u = (int)((x - cuts) >> 8), pj = u / hk, kh = u - pj * hk;
+      const KvJob j = job_from_l2(p.jobs + pj);
+      if (tl >= p.tpt || tok >= j.ntok) continue;
+      row = j.tok0 + tok;
+      hq = kh * p.ratio + hl;
+      int i = row;   // single tokens: request i has row i
+      if (!(row < n && a.b.q_start[row] == row && a.b.q_start[row + 1] == row + 1)) {
+        int lo = 0, hi = n;
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (a.b.q_start[mid] <= row) lo = mid; else hi = mid;
+        }
+        i = lo;
+      }
+      const int j0 = __ldcg(p.job0 + i), q0 = a.b.q_start[i];
+      if (j0 >= 0 && q0 >= 0 && row >= q0) {
+        const KvJob o = job_from_l2(p.jobs + min(j0 + (row - q0) / w2, hd.jobs - 1));
+        const int t = row - o.tok0;
+        if (t >= 0 && t < o.ntok) own = parts_of(o, kh, hk, hd);
+        ro = (t >= p.tpt ? 128 + (t - p.tpt) * p.ratio : t * p.ratio) + hl;
+      }
+      pre = parts_of(j, kh, hk, hd);
+    }
+    join_row<D, HALF>(a, p, pre, rr, own, ro, row, hq, lane);
+  }
+}
+
+template <int D, bool HALF>
+__global__ void __launch_bounds__(256) k_kv_join(const __grid_constant__ KvAttendArgs a,
+                                                 const __grid_constant__ KvPlan p) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  join_rows<D, HALF>(a, p, *p.head, (int)blockIdx.x * 8 + (int)(threadIdx.x >> 5), (int)gridDim.x * 8);
+}
+
 // ------------------------------------------------------------------ the kernel
 
 // Tiles t0 .. t1 - 1 of a job and head.
@@ -655,8 +847,7 @@ struct Walk {
   int kind;
   Seg a, b;
 
-  __device__ Walk(const KvPlan& p, int n_kv_heads) {
-    const KvStart s = p.start[blockIdx.x];
+  __device__ Walk(const KvPlan& p, const KvStart& s, int n_kv_heads) {
     jobs = p.jobs;
     heads = n_kv_heads;
     rem = s.rem;
@@ -729,7 +920,9 @@ struct Lay {
   static constexpr int NBAR = 2 * NST + 13 + 2 * NR;
   static constexpr int ML = MISC + 384;           // float2 [128]
   static constexpr int RUNS = ML + 1024;          // Run [NR]
-  static constexpr int SMEM = RUNS + NR * (int)sizeof(Run);
+  static constexpr int START = RUNS + NR * (int)sizeof(Run);   // KvStart, KvHead
+  static constexpr int SMEM = START + (int)sizeof(KvStart) + (int)sizeof(KvHead);
+  static_assert((int)sizeof(PlanSmem) <= MISC, "the plan's memory is the tiles'");
 };
 
 // The loads' order is that of first use: K of each stream's first tile, then for
@@ -763,6 +956,8 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
                  SFULL = QFULL + 32, PFULL = QFULL + 48, OFULL = QFULL + 64, OEMPTY = QFULL + 80,
                  MEET = QFULL + 96, RFULL = QFULL + 104, REMPTY = RFULL + 8 * NR;
   Run* const runs = reinterpret_cast<Run*>(sm + L::RUNS);
+  KvStart* const start = reinterpret_cast<KvStart*>(sm + L::START);
+  KvHead* const head = reinterpret_cast<KvHead*>(sm + L::START + sizeof(KvStart));
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(sm + L::MISC + 8 * L::NBAR);
   volatile int* lost = reinterpret_cast<volatile int*>(sm + L::MISC + 8 * L::NBAR + 4);
   static_assert(8 * L::NBAR + 8 <= 384, "barriers");
@@ -795,14 +990,28 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
   __syncthreads();
   tc_after();
   const uint32_t tmem = *s_tmem;
-  asm volatile("griddepcontrol.wait;" ::: "memory");   // the plan
+  const unsigned generation = *reinterpret_cast<volatile unsigned*>(&p.meet[1]);   // (nobody moves it before this CTA has arrived)
+  if (p.planned) {
+    if (tid == 0) {
+      *start = p.start[blockIdx.x];
+      *head = *p.head;
+    }
+  } else {
+    make_plan(a.b, p, a.c.n_kv_heads, *reinterpret_cast<PlanSmem*>(sm), false, start, head);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (copies into the same memory follow)
+  }
+  __syncthreads();
   asm volatile("griddepcontrol.launch_dependents;");
 
+  auto drain = [] {   // copies in flight end before the CTA's memory is another's
+    const long long t = clock64();
+    while (clock64() - t < 20000000ll) {}
+  };
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == 10) {
       // ---------------- runs
-      Walk w(p, a.c.n_kv_heads);
+      Walk w(p, *start, a.c.n_kv_heads);
       for (uint32_t k = 0; !*lost; k++) {
         w.next();
         // the lane's page: stream lane / 16, its tile (lane / 8) % 2
@@ -973,6 +1182,12 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
         qn += split ? 1 : 2;
         done++;
       }
+    }
+    __syncthreads();   // the streams are done
+    if (*lost) drain();
+    if (warp == 8) {
+      tc_after();
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
     }
   } else {
     // ---------------- softmax, a thread a row
@@ -1210,181 +1425,32 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
         mbar_arrive(REMPTY + 8 * (k % NR));
       }
     }
-  }
-  __syncthreads();
-  if (*lost) {   // copies in flight end before the CTA's memory is another's
-    const long long t = clock64();
-    while (clock64() - t < 20000000ll) {}
-  }
-  if (warp == 8) {
-    tc_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
-  }
-}
-
-// ------------------------------------------------------------------ joining
-
-// Where the parts of a job and head are: whole in its place among all rows (one
-// part, last < first), or in CTAs first .. last.
-struct Parts {
-  int c0, first, last, count;
-};
-
-__device__ __forceinline__ Parts parts_of(const KvJob& j, int head, int n_kv_heads, const KvHead& hd) {
-  Parts r{0, 0, 0, 0};
-  if (j.nt <= 0) return r;
-  const int cost = job_cost(j.nt, j.flags);
-  const int64_t u0 = j.cost * n_kv_heads + (int64_t)head * cost;
-  const int64_t c0 = quotient(u0, hd.per), c1 = quotient(u0 + cost - 1, hd.per);
-  int t0, t1;
-  r.c0 = (int)c0;
-  r.first = (int)(segment(u0, cost, j.flags, j.nt, hd.per, c0, t0, t1) ? c0 : c0 + 1);
-  r.last = (int)(segment(u0, cost, j.flags, j.nt, hd.per, c1, t0, t1) ? c1 : c1 - 1);
-  r.count = max(r.last - r.first + 1, 1);
-  if (r.count == 1) r.last = r.first - 1;
-  return r;
-}
-
-__device__ __forceinline__ KvJob job_from_l2(const KvJob* j) {
-  KvJob r;
-  const int4* s = reinterpret_cast<const int4*>(j);
-  int4* d = reinterpret_cast<int4*>(&r);
-#pragma unroll
-  for (int k = 0; k < 3; k++) d[k] = __ldcg(s + k);
-  return r;
-}
-
-// One row (token, head) from its parts: x's (row rx of the 256 if cut, else at
-// home), then y's.  A lane takes the log sum of a part, the warp their largest
-// and the weights, and the rows of several parts are on their way at once.
-template <int D, bool HALF>
-__device__ __forceinline__ void join_row(const KvAttendArgs& a, const KvPlan& p, const Parts& x, int rx, const Parts& y, int ry,
-                                         int64_t row, int hq, int lane) {
-  constexpr int E = D / 32;
-  const int64_t home = row * a.n_heads + hq, all = (int64_t)a.b.n_tokens * a.n_heads;
-  const int count = x.count + y.count;
-  float m = -INFINITY, l = 0.0f, o[E];
-#pragma unroll
-  for (int e = 0; e < E; e++) o[e] = 0.0f;
-  for (int base = 0; base < count; base += 32) {
-    const int k = base + lane;
-    const float* src = nullptr;
-    float s = -INFINITY;
-    if (k < count) {
-      const Parts& q = k < x.count ? x : y;
-      const int c = q.first + (k < x.count ? k : k - x.count);
-      const bool whole = q.last < q.first;
-      const int64_t at = whole ? (k < x.count ? 0 : all) + home
-                               : ((int64_t)c * 2 + (c == q.c0 ? 1 : 0)) * 256 + (k < x.count ? rx : ry);
-      s = (whole ? p.home_lse : p.part_lse)[at];
-      src = (whole ? p.home : p.part) + at * D;
-    }
-    float big = s;
-#pragma unroll
-    for (int z = 16; z; z >>= 1) big = fmaxf(big, __shfl_xor_sync(~0u, big, z));
-    const float m2 = fmaxf(m, big);
-    const float wt = s == -INFINITY ? 0.0f : ex2(__fsub_rn(s, m2));
-    const float f = m == -INFINITY ? 0.0f : ex2(__fsub_rn(m, m2));
-    float sum = wt;
-#pragma unroll
-    for (int z = 16; z; z >>= 1) sum = __fadd_rn(sum, __shfl_xor_sync(~0u, sum, z));
-    l = fmaf(l, f, sum);
-#pragma unroll
-    for (int e = 0; e < E; e++) o[e] = __fmul_rn(o[e], f);
-    m = m2;
-    const int here = min(32, count - base);
-    for (int q = 0; q < here; q += 8) {
-      float w8[8], v[8][E];
-#pragma unroll
-      for (int z = 0; z < 8; z++) {   // (past the last part: weight 0, the last one's row)
-        const int from = min(q + z, here - 1);
-        const float w = __shfl_sync(~0u, wt, from);
-        w8[z] = q + z < here ? w : 0.0f;
-        const float* r = reinterpret_cast<const float*>(__shfl_sync(~0u, reinterpret_cast<unsigned long long>(src), from)) + lane * E;
-        if constexpr (E == 4) {
-          const float4 t = *reinterpret_cast<const float4*>(r);
-          v[z][0] = t.x; v[z][1] = t.y; v[z][2] = t.z; v[z][3] = t.w;
+    __syncthreads();
+    if (*lost) drain();
+    const KvHead hd = *head;
+    if (p.join_here && (hd.cuts > 0 || hd.prefix_jobs > 0)) {
+      // every CTA's parts are there when all have met (they all run at once: a cooperative launch)
+      if (tid == 0) {
+        __threadfence();
+        if (atomicAdd(&p.meet[0], 1u) == gridDim.x - 1) {
+          p.meet[0] = 0;
+          __threadfence();
+          atomicAdd(&p.meet[1], 1u);
         } else {
-          const float2 t = *reinterpret_cast<const float2*>(r);
-          v[z][0] = t.x; v[z][1] = t.y;
+          const long long t = clock64();
+          while (*reinterpret_cast<volatile unsigned*>(&p.meet[1]) == generation) {
+            if (clock64() - t > (1ll << 37)) {   // (a minute)
+              *reinterpret_cast<volatile int32_t*>(p.err) = 1;
+              break;
+            }
+          }
         }
+        __threadfence();
       }
-#pragma unroll
-      for (int z = 0; z < 8; z++)
-#pragma unroll
-        for (int e = 0; e < E; e++) o[e] = w8[z] == 0.0f ? o[e] : fmaf(w8[z], v[z][e], o[e]);
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      join_rows<D, HALF>(a, p, hd, (int)blockIdx.x + warp * (int)gridDim.x, (int)gridDim.x * 8);
     }
   }
-  const float inv = l == 0.0f ? 0.0f : __fdiv_rn(1.0f, l);
-  uint16_t* out = static_cast<uint16_t*>(a.out) + row * a.o_ts + hq * a.o_hs + lane * E;
-  uint32_t z[E / 2];
-#pragma unroll
-  for (int e = 0; e < E; e += 2) z[e / 2] = pack2<HALF>(__fmul_rn(o[e], inv), __fmul_rn(o[e + 1], inv));
-  if constexpr (E == 4) *reinterpret_cast<uint2*>(out) = make_uint2(z[0], z[1]);
-  else *reinterpret_cast<uint32_t*>(out) = z[0];
-  if (a.lse && lane == 0)
-    a.lse[home] = l == 0.0f ? -INFINITY : __fmul_rn(__fadd_rn(m, __log2f(l)), 0.6931471805599453f);
-}
-
-// Rows that have parts, a warp a row, a CTA for 8 of a job's 256: of the jobs that
-// a share's end cut, and of shared groups, whose rows have a prefix job and an own
-// one.  The parts' order is the keys', so the result does not depend on when they
-// came.  What the plan says is read before the attention kernel has ended (the
-// plan had, when it let this one start).
-template <int D, bool HALF>
-__global__ void __launch_bounds__(256) k_kv_join(const __grid_constant__ KvAttendArgs a,
-                                                 const __grid_constant__ KvPlan p) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int hk = a.c.n_kv_heads, w2 = 2 * p.tpt, n = a.b.n_req;
-  KvHead hd;
-  const int4 h0 = __ldcg(reinterpret_cast<const int4*>(p.head)), h1 = __ldcg(reinterpret_cast<const int4*>(p.head) + 1);
-  memcpy(&hd, &h0, 16);
-  memcpy(reinterpret_cast<char*>(&hd) + 16, &h1, 16);
-  bool waited = false;
-  auto wait = [&]() {
-    if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
-    waited = true;
-  };
-  const int64_t cuts = (int64_t)hd.cuts * 32, tasks = cuts + (int64_t)hd.prefix_jobs * hk * 32;
-  for (int64_t task = blockIdx.x; task < tasks; task += gridDim.x) {
-    const int rr = (int)(task & 31) * 8 + warp, r = rr & 127, tl = r / p.ratio, hl = r - tl * p.ratio;
-    const int tok = (rr >> 7) * p.tpt + tl;
-    if (task < cuts) {
-      const int4* c = reinterpret_cast<const int4*>(p.cut + (task >> 5));
-      const int4 c0 = __ldcg(c), c1 = __ldcg(c + 1);
-      if (tl >= p.tpt || tok >= c0.y) continue;
-      const Parts x{c0.w, c1.x, c1.y, c1.y - c1.x + 1}, none{0, 0, 0, 0};
-      wait();
-      join_row<D, HALF>(a, p, x, rr, none, 0, (int64_t)c0.x + tok, c0.z * p.ratio + hl, lane);
-      continue;
-    }
-    const int u = (int)((task - cuts) >> 5), pj = u / hk, kh = u - pj * hk;
-    const KvJob pre = job_from_l2(p.jobs + pj);
-    if (tl >= p.tpt || tok >= pre.ntok) continue;
-    const int row = pre.tok0 + tok;
-    int i = row;   // single tokens: request i has row i
-    if (!(row < n && __ldcg(a.b.q_start + row) == row && __ldcg(a.b.q_start + row + 1) == row + 1)) {
-      int lo = 0, hi = n;
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (__ldcg(a.b.q_start + mid) <= row) lo = mid; else hi = mid;
-      }
-      i = lo;
-    }
-    const int j0 = __ldcg(p.job0 + i), q0 = __ldcg(a.b.q_start + i);
-    Parts own{0, 0, 0, 0};
-    int ro = 0;
-    if (j0 >= 0 && q0 >= 0 && row >= q0) {
-      const KvJob j = job_from_l2(p.jobs + min(j0 + (row - q0) / w2, hd.jobs - 1));
-      const int t = row - j.tok0;
-      if (t >= 0 && t < j.ntok) own = parts_of(j, kh, hk, hd);
-      ro = (t >= p.tpt ? 128 + (t - p.tpt) * p.ratio : t * p.ratio) + hl;
-    }
-    const Parts x = parts_of(pre, kh, hk, hd);
-    wait();
-    join_row<D, HALF>(a, p, x, rr, own, ro, row, kh * p.ratio + hl, lane);
-  }
-  wait();   // (no CTA ends before the attention kernel: the next call's plan waits for this one)
 }
 
 // ------------------------------------------------------------------ host
@@ -1416,21 +1482,6 @@ bool encode(CUtensorMap* m, bool half, const void* p, int rank, const cuuint64_t
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <class... P, class... A>
-cudaError_t launch_after(void (*k)(P...), unsigned grid, int threads, size_t smem, cudaStream_t st, A&&... args) {
-  cudaLaunchConfig_t c = {};
-  c.gridDim = dim3(grid);
-  c.blockDim = dim3(threads);
-  c.dynamicSmemBytes = smem;
-  c.stream = st;
-  cudaLaunchAttribute at;
-  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at.val.programmaticStreamSerializationAllowed = 1;
-  c.attrs = &at;
-  c.numAttrs = 1;
-  return cudaLaunchKernelEx(&c, k, std::forward<A>(args)...);
-}
-
 size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // The workspace; with ws NULL only its size.
@@ -1446,6 +1497,7 @@ size_t carve(const KvAttendArgs& a, int ctas, unsigned char* ws, KvPlan& p) {
     if (ws) ptr = reinterpret_cast<std::remove_reference_t<decltype(ptr)>>(ws + o);
     o = up(o + count * sizeof(*ptr));
   };
+  take(p.meet, 2);   // (first: in its place whatever the call's sizes)
   take(p.head, 1);
   take(p.jobs, (size_t)p.cap + 1);
   take(p.job0, n);
@@ -1460,24 +1512,43 @@ size_t carve(const KvAttendArgs& a, int ctas, unsigned char* ws, KvPlan& p) {
   return o;
 }
 
+constexpr int64_t JOIN_HERE = 2048;   // rows up to which the attention kernel joins parts itself
+
 template <int D, bool HALF>
 cudaError_t run(const KvAttendArgs& a, const KvPlan& p, const CUtensorMap* m, cudaStream_t st) {
   using L = Lay<D>;
   static_assert(D == 64 || D == 128, "two head sizes");
-  cudaError_t e = cudaFuncSetAttribute(k_kv_attend<D, HALF>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM);
+  auto k = k_kv_attend<D, HALF>;
+  cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM);
   if (e != cudaSuccess) return e;
-  // the register split below (2 x 208 + 88 a thread of each four warps) has to be within what the CTA starts with
+  // the kernel's register split (2 x 208 + 88 a thread of each four warps) has to be within what a CTA starts with
   static const int regs = [] {
     cudaFuncAttributes f;
     return cudaFuncGetAttributes(&f, k_kv_attend<D, HALF>) == cudaSuccess ? f.numRegs : 0;
   }();
   if (regs * 3 < 2 * 208 + 88) return cudaErrorInvalidKernelImage;
-  e = launch_after(k_kv_attend<D, HALF>, p.ctas, NT_ATT, L::SMEM, st, m[0], m[1], m[2], m[3], a, p);
-  if (e != cudaSuccess) return e;
-  // no more CTAs than the GPU holds at once
+  cudaLaunchConfig_t c = {};
+  c.gridDim = dim3(p.ctas);
+  c.blockDim = dim3(NT_ATT);
+  c.dynamicSmemBytes = L::SMEM;
+  c.stream = st;
+  cudaLaunchAttribute at;
+  c.attrs = &at;
+  c.numAttrs = p.join_here ? 1 : 0;
+  at.id = cudaLaunchAttributeCooperative;   // (its CTAs wait for one another before they join parts)
+  at.val.cooperative = 1;
+  e = cudaLaunchKernelEx(&c, k, m[0], m[1], m[2], m[3], a, p);
+  if (e != cudaSuccess || p.join_here) return e;
+  // a warp a row, no more than the GPU holds at once
   const int64_t jobs = a.b.n_groups ? std::min<int64_t>(a.b.n_tokens / (2 * p.tpt) + a.b.n_groups, p.cap) : 0;
-  const int64_t tasks = (p.ctas + jobs * a.c.n_kv_heads) * 32;
-  return launch_after(k_kv_join<D, HALF>, (unsigned)std::min<int64_t>(tasks, (int64_t)p.ctas * 16), 256, 0, st, a, p);
+  const int64_t rows = (p.ctas + jobs * a.c.n_kv_heads) * 256;
+  c.gridDim = dim3((unsigned)std::min<int64_t>((rows + 7) / 8, (int64_t)p.ctas * 8));
+  c.blockDim = dim3(256);
+  c.dynamicSmemBytes = 0;
+  c.numAttrs = 1;
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  return cudaLaunchKernelEx(&c, k_kv_join<D, HALF>, a, p);
 }
 
 }  // namespace
@@ -1504,12 +1575,17 @@ cudaError_t launch_kv_attend(const KvAttendArgs& a, void* ws, int32_t* err, int 
   if (!encode(&m[0], half, a.c.k, 4, ks, kst, kbox) || !encode(&m[1], half, a.c.v, 4, ks, kst, kbox) ||
       !encode(&m[2], half, a.q, 3, qs, qst, qbox) || !encode(&m[3], half, a.q, 3, qs, qst, qbox1))
     return cudaErrorInvalidValue;
-  const size_t psm = PLAN_JOBS * sizeof(KvJob) + (size_t)4 * PLAN_GROUPS * 8 + (size_t)(3 * PLAN_GROUPS + 1) * 4;
-  cudaError_t e = cudaFuncSetAttribute(k_kv_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)psm);
-  if (e != cudaSuccess) return e;
-  k_kv_plan<<<1, a.b.n_req <= 256 && a.b.n_groups <= 256 && p.cap <= PLAN_JOBS ? 256 : NT_PLAN, psm, st>>>(a.b, p, a.c.n_kv_heads);
-  e = cudaGetLastError();
-  if (e != cudaSuccess) return e;
+  // up to PLAN_JOBS jobs every CTA finds its share by itself, in the time that a kernel before it and its start would
+  // take; more are one CTA's work for all
+  p.planned = p.cap > PLAN_JOBS || a.b.n_groups > PLAN_GROUPS;
+  p.join_here = (int64_t)a.b.n_tokens * a.n_heads <= JOIN_HERE;
+  if (p.planned) {
+    cudaError_t e = cudaFuncSetAttribute(k_kv_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(PlanSmem));
+    if (e != cudaSuccess) return e;
+    k_kv_plan<<<1, NT_PLAN, sizeof(PlanSmem), st>>>(a.b, p, a.c.n_kv_heads);
+    e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+  }
   if (D == 128) return half ? run<128, true>(a, p, m, st) : run<128, false>(a, p, m, st);
   return half ? run<64, true>(a, p, m, st) : run<64, false>(a, p, m, st);
 }
