@@ -1448,14 +1448,9 @@ rs_status kv_attend(rs_ctx* ctx, const rs_kv_cache* cache, const rs_kv_batch* ba
   }
   if (*static_cast<volatile int32_t*>(ctx->kv_err)) {
     *ctx->kv_err = 0;
-    release(ctx->kv_ws);   // (its counters may be in between)
     return fail(ctx, RS_ERR_TIMEOUT, "an earlier kv_attend gave up waiting for its own copies or products");
   }
-  const size_t bytes = kv_attend_bytes(a, ctx->sms);
-  if (bytes > ctx->kv_ws.n) {
-    if ((r = ensure(ctx, ctx->kv_ws, bytes, "attention workspace")) != RS_OK) return r;
-    CK(cudaMemsetAsync(ctx->kv_ws.p, 0, 256, ctx->st), "memset");   // its counters
-  }
+  if ((r = ensure(ctx, ctx->kv_ws, kv_attend_bytes(a, ctx->sms), "attention workspace")) != RS_OK) return r;
   CK(launch_kv_attend(a, ctx->kv_ws.p, ctx->kv_err, ctx->sms, ctx->st), "attention launch");
   return RS_OK;
 }

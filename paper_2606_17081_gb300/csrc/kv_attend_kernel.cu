@@ -20,7 +20,7 @@
 
 #include <algorithm>
 #include <climits>
-#include <cstring>
+#include <type_traits>
 
 #include "rs_internal.h"
 
@@ -53,7 +53,7 @@ struct __align__(16) KvJob {
   int32_t lim0;         // keys that the first token sees; the next see one more each
   int32_t flags;
   int64_t cost;         // of the jobs before, for one kv head
-  int64_t reserved0;
+  int64_t rows;         // of a prefix job: tokens of the prefix jobs before
 };
 
 // A job and head that a share's end cuts, at the share's end that cuts it first.
@@ -67,7 +67,10 @@ struct __align__(16) KvCut {
 
 struct KvHead {
   int64_t total, per;   // cost of all jobs and heads, of one CTA
-  int32_t jobs, prefix_jobs, cuts, reserved0;
+  int32_t jobs, prefix_jobs;
+  int32_t shared;       // tokens of the prefix jobs
+  int32_t cuts, cut_rows;   // cut jobs, and the most rows of one
+  int32_t reserved0;
 };
 
 struct __align__(16) KvStart {
@@ -77,7 +80,6 @@ struct __align__(16) KvStart {
 };
 
 struct KvPlan {
-  unsigned* meet;       // [2] CTAs that have arrived, times that all have; 0 at first
   KvHead* head;
   KvJob* jobs;          // [cap + 1]
   int32_t* job0;        // [n_req] first own job, or -1
@@ -95,7 +97,6 @@ struct KvPlan {
   int32_t tpt;          // tokens of 128 rows
   int32_t ratio;        // heads of a kv head
   int32_t planned;      // the plan is there before the attention kernel begins
-  int32_t join_here;    // the attention kernel joins the parts itself
 };
 
 namespace {
@@ -106,31 +107,41 @@ __device__ __forceinline__ int clampi(int64_t x, int lo, int hi) {
   return (int)(x < lo ? lo : x > hi ? hi : x);
 }
 
+template <class Int>
 struct JobSum {
-  int64_t count, cost;
+  Int count, cost, rows;   // jobs, their cost, tokens of prefix jobs
 };
 
-// Exclusive block sum of x and its total; sm: one entry a warp, not the one of the
-// sum before.
-__device__ JobSum block_scan(JobSum x, JobSum* sm, JobSum& total) {
+// Exclusive sum of x over the CTA's first `width` threads (the others have 0), and
+// its total; sm: one entry a warp, not the one of the sum before.
+template <class Int>
+__device__ JobSum<Int> block_scan(JobSum<Int> x, JobSum<Int>* sm, int width, JobSum<Int>& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  auto scan = [&](JobSum s) {
+  auto scan = [&](JobSum<Int> s) {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int64_t y = __shfl_up_sync(~0u, s.count, o);
-      const int64_t z = __shfl_up_sync(~0u, s.cost, o);
-      if (lane >= o) { s.count += y; s.cost += z; }
+      const Int x = __shfl_up_sync(~0u, s.count, o), y = __shfl_up_sync(~0u, s.cost, o), z = __shfl_up_sync(~0u, s.rows, o);
+      if (lane >= o) { s.count += x; s.cost += y; s.rows += z; }
     }
     return s;
   };
-  const JobSum s = scan(x);
-  if (lane == 31) sm[warp] = s;
+  JobSum<Int> s{0, 0, 0};
+  if (warp * 32 < width) {
+    s = scan(x);
+    if (lane == 31) sm[warp] = s;
+  }
   __syncthreads();
-  const JobSum w = lane < (int)(blockDim.x >> 5) ? sm[lane] : JobSum{0, 0}, ws = scan(w);
+  if (width <= 32) {
+    total = sm[0];
+    return JobSum<Int>{s.count - x.count, s.cost - x.cost, s.rows - x.rows};
+  }
+  const JobSum<Int> w = lane * 32 < width ? sm[lane] : JobSum<Int>{0, 0, 0}, ws = scan(w);
   total.count = __shfl_sync(~0u, ws.count, 31);
   total.cost = __shfl_sync(~0u, ws.cost, 31);
-  return JobSum{__shfl_sync(~0u, ws.count - w.count, warp) + s.count - x.count,
-                __shfl_sync(~0u, ws.cost - w.cost, warp) + s.cost - x.cost};
+  total.rows = __shfl_sync(~0u, ws.rows, 31);
+  return JobSum<Int>{__shfl_sync(~0u, ws.count - w.count, warp) + s.count - x.count,
+                     __shfl_sync(~0u, ws.cost - w.cost, warp) + s.cost - x.cost,
+                     __shfl_sync(~0u, ws.rows - w.rows, warp) + s.rows - x.rows};
 }
 
 struct ReqLens {
@@ -168,10 +179,10 @@ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
 // A plan's working memory.
 struct PlanSmem {
   KvJob job[PLAN_JOBS];
-  unsigned long long sum[4 * PLAN_GROUPS];
+  uint64_t sum[4 * PLAN_GROUPS];
   int32_t start[PLAN_GROUPS + 1], prefix[PLAN_GROUPS], gjob[PLAN_GROUPS];
-  JobSum scan[2][32];
-  int32_t cuts;
+  JobSum<int64_t> scan[2][32];
+  int32_t cuts, cut_rows;
 };
 
 // By a whole CTA: whether each group's prefix pays as one job for all its rows,
@@ -179,26 +190,31 @@ struct PlanSmem {
 // all that counts here (a few dependent reads and block sums): lengths are read
 // once at up to a request a thread, group sums and jobs live in shared memory at
 // ordinary sizes.  Starts that decrease can ask for more jobs than there is room
-// for: those get no work.
+// for: then there is no work at all.
 //   all = true: one CTA for everybody, starts into p.start.
 //   all = false (at most PLAN_JOBS jobs and PLAN_GROUPS groups): every CTA for
 //     itself, its start into *mine and the jobs of its share into p.jobs; what the
 //     joining needs is written by CTA 0.
+// Int: wide enough for all jobs' cost.
+template <class Int>
 __device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p, int n_kv_heads, PlanSmem& ps, bool all_ctas,
-                                          KvStart* own_start, KvHead* own_head) {
+                                          KvStart* own_start) {
+  using Sum = JobSum<Int>;
+  Sum(*scan)[32] = reinterpret_cast<Sum(*)[32]>(ps.scan);
   const bool writer = all_ctas || blockIdx.x == 0;
   KvJob* s_job = ps.job;
-  unsigned long long* s_sum = ps.sum;
+  using Acc = std::conditional_t<sizeof(Int) == 4, unsigned, unsigned long long>;
+  Acc* s_sum = reinterpret_cast<Acc*>(ps.sum);
   int32_t *s_start = ps.start, *s_prefix = ps.prefix, *s_gjob = ps.gjob;
   const int tid = threadIdx.x, lane = tid & 31, nth = blockDim.x, n = b.n_req, G = b.n_groups;
   const int w2 = 2 * p.tpt;
   const bool few = G <= PLAN_GROUPS;
-  unsigned long long* sum = few ? s_sum : p.gsum;
+  Acc* sum = few ? s_sum : reinterpret_cast<Acc*>(p.gsum);
   const int32_t* gstart = few ? s_start : b.group_start;
   const int32_t* glen = few ? s_prefix : b.prefix_len;
   int32_t* gjob = few ? s_gjob : p.gjob;
 
-  auto of = [&](int x) { return few ? s_sum[x] : __ldcg(p.gsum + x); };
+  auto of = [&](int x) { return few ? s_sum[x] : __ldcg(sum + x); };
   auto prefix_keys = [&](int g) { return (int)min((int64_t)(max(glen[g], 0) & ~15), (int64_t)b.max_blocks * 16); };
   auto rows_at = [&](int i) { return clampi(b.q_start[i], 0, b.n_tokens); };
   auto lens = [&](int i) {
@@ -217,16 +233,20 @@ __device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p,
     }
     return lo;
   };
+  // what every later step goes by, all on its way at once
+  const int g0 = few && tid <= G && G > 0 ? b.group_start[tid] : 0, p0 = few && tid < G ? b.prefix_len[tid] : 0;
   ReqLens mine{0, 0, 0, -1};   // of request tid
   if (tid < n) mine = lens(tid);
   const int q_end = n > 0 ? rows_at(n) : 0;
-  if (tid == 0) ps.cuts = 0;
-  JobSum jobs{0, 0}, total;
+  if (tid == 0) ps.cuts = ps.cut_rows = 0;
+  Sum jobs{0, 0, 0}, total;
   int turn = 0;
   if (G > 0) {
     if (few) {
-      for (int g = tid; g <= G; g += nth) s_start[g] = b.group_start[g];
-      for (int g = tid; g < G; g += nth) s_prefix[g] = b.prefix_len[g];
+      if (tid <= G) s_start[tid] = g0;
+      if (tid < G) s_prefix[tid] = p0;
+      for (int g = tid + nth; g <= G; g += nth) s_start[g] = b.group_start[g];
+      for (int g = tid + nth; g < G; g += nth) s_prefix[g] = b.prefix_len[g];
     }
     // of each group: its requests' costs without and with a shared prefix, whether
     // some row sees less than the prefix, the longest context
@@ -240,10 +260,10 @@ __device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p,
     r.g = group(i);
     return r;
   };
-  auto put = [&](JobSum at, KvJob j) {
+  auto put = [&](Sum at, KvJob j) {
     if (at.count >= p.cap) return;
     j.cost = at.cost;
-    j.reserved0 = 0;
+    j.rows = at.rows;
     if (writer) p.jobs[at.count] = j;
     if (at.count < PLAN_JOBS) s_job[at.count] = j;
   };
@@ -260,10 +280,10 @@ __device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p,
       const unsigned with = __reduce_add_sync(peers, (unsigned)min((int64_t)rt * job_cost(tiles(seen - P), fl), (int64_t)top));
       const unsigned less = __reduce_or_sync(peers, r.kv - r.q + 1 < P), most = __reduce_max_sync(peers, (unsigned)r.kv);
       if (lane == __ffs(peers) - 1) {
-        atomicAdd(&sum[4 * g], (unsigned long long)apart);
-        atomicAdd(&sum[4 * g + 1], (unsigned long long)with);
+        atomicAdd(&sum[4 * g], (Acc)apart);
+        atomicAdd(&sum[4 * g + 1], (Acc)with);
         if (less) sum[4 * g + 2] = 1;
-        atomicMax(&sum[4 * g + 3], (unsigned long long)most);
+        atomicMax(&sum[4 * g + 3], (Acc)most);
       }
     }
     __syncthreads();
@@ -274,25 +294,28 @@ __device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p,
     for (int base = 0; base < G; base += nth) {
       const int g = base + tid;
       int cnt = 0, t0 = 0, t1 = 0, P = 0, first = 0, last_flags = 0;
-      JobSum x{0, 0};
+      Sum x{0, 0, 0};
       if (g < G) {
         first = clampi(gstart[g], 0, n);
         const int last = clampi(gstart[g + 1], 0, n);
         t0 = rows_at(first);
         t1 = rows_at(max(first, last));
         const int rt = t1 > t0 ? (t1 - t0 + w2 - 1) / w2 : 0;
-        P = (int)min((unsigned long long)prefix_keys(g), of(4 * g + 3));   // (what nobody has written yet is not read)
+        P = (int)min((Acc)prefix_keys(g), of(4 * g + 3));   // (what nobody has written yet is not read)
         last_flags = t1 - t0 - (rt - 1) * w2 > p.tpt ? JOB_WIDE : 0;
-        x.cost = (int64_t)(rt - 1) * job_cost(tiles(P), JOB_WIDE) + job_cost(tiles(P), last_flags);
-        if (P > 0 && first < last && rt > 0 && of(4 * g + 1) + x.cost + W_NARROW / 4 * (t1 - t0) < of(4 * g)) cnt = rt;
+        x.cost = (Int)(rt - 1) * job_cost(tiles(P), JOB_WIDE) + job_cost(tiles(P), last_flags);
+        if (P > 0 && first < last && rt > 0 && (int64_t)of(4 * g + 1) + x.cost + W_NARROW / 4 * (t1 - t0) < (int64_t)of(4 * g)) cnt = rt;
         if (cnt == 0) x.cost = 0;
         x.count = cnt;
+        x.rows = cnt > 0 ? t1 - t0 : 0;
       }
-      JobSum at = block_scan(x, ps.scan[turn ^= 1], total);
+      Sum at = block_scan(x, scan[turn ^= 1], min(nth, G - base), total);
       at.count += jobs.count;
       at.cost += jobs.cost;
+      at.rows += jobs.rows;
       jobs.count += total.count;
       jobs.cost += total.cost;
+      jobs.rows += total.rows;
       if (g < G) {
         gjob[g] = cnt > 0 && at.count + cnt <= p.cap ? (int32_t)at.count : -1;
         KvJob j = {};
@@ -306,18 +329,19 @@ __device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p,
           put(at, j);
           at.count++;
           at.cost += job_cost(j.nt, j.flags);
+          at.rows += j.ntok;
         }
       }
     }
     __syncthreads();   // gjob
   }
-  const int prefix_jobs = (int)min(jobs.count, (int64_t)p.cap);
+  const int prefix_jobs = (int)min((int64_t)jobs.count, (int64_t)p.cap);
   // the requests' own jobs
   for (int base = 0; base < n; base += nth) {
     const int i = base + tid;
     ReqLens r{0, 0, 0, -1};
     int key0 = 0, alone = 1;
-    JobSum x{0, 0};
+    Sum x{0, 0, 0};
     if (i < n) {
       r = request(i);
       if (r.g >= 0 && gjob[r.g] >= 0) {
@@ -347,7 +371,7 @@ __device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p,
       const int src = __ffs(todo) - 1;
       const int sc = __shfl_sync(~0u, (int)x.count, src), sq = __shfl_sync(~0u, r.q, src), sk = __shfl_sync(~0u, r.kv, src);
       const int s1 = __shfl_sync(~0u, key0, src), sa = __shfl_sync(~0u, alone, src);
-      int64_t c = 0;
+      Int c = 0;
       for (int k = lane; k < sc; k += 32) {
         const KvJob j = job(k, 0, 0, sq, sk, s1, sa);
         c += job_cost(j.nt, j.flags);
@@ -356,7 +380,7 @@ __device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p,
       for (int o = 16; o; o >>= 1) c += __shfl_xor_sync(~0u, c, o);
       if (lane == src) x.cost = c;
     }
-    JobSum at = block_scan(x, ps.scan[turn ^= 1], total);
+    Sum at = block_scan(x, scan[turn ^= 1], min(nth, n - base), total);
     at.count += jobs.count;
     at.cost += jobs.cost;
     jobs.count += total.count;
@@ -368,18 +392,18 @@ __device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p,
       const int sc = __shfl_sync(~0u, (int)x.count, src), si = __shfl_sync(~0u, i, src);
       const int s0 = __shfl_sync(~0u, r.q0, src), sq = __shfl_sync(~0u, r.q, src), sk = __shfl_sync(~0u, r.kv, src);
       const int s1 = __shfl_sync(~0u, key0, src), sa = __shfl_sync(~0u, alone, src);
-      JobSum sat{__shfl_sync(~0u, at.count, src), __shfl_sync(~0u, at.cost, src)};
+      Sum sat{__shfl_sync(~0u, at.count, src), __shfl_sync(~0u, at.cost, src), 0};
       for (int k0 = 0; k0 < sc; k0 += 32) {
         const int k = k0 + lane;
         const KvJob j = job(min(k, sc - 1), si, s0, sq, sk, s1, sa);
-        const int64_t c = k < sc ? job_cost(j.nt, j.flags) : 0;
-        int64_t before = c;
+        const Int c = k < sc ? job_cost(j.nt, j.flags) : 0;
+        Int before = c;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-          const int64_t y = __shfl_up_sync(~0u, before, o);
+          const Int y = __shfl_up_sync(~0u, before, o);
           if (lane >= o) before += y;
         }
-        if (k < sc) put(JobSum{sat.count + k, sat.cost + before - c}, j);
+        if (k < sc) put(Sum{sat.count + k, sat.cost + before - c, 0}, j);
         sat.cost += __shfl_sync(~0u, before, 31);
       }
     }
@@ -391,11 +415,11 @@ __device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p,
     j.tok0 = q_end + k * w2;
     j.ntok = min(w2, b.n_tokens - j.tok0);
     j.flags = JOB_ALONE | (j.ntok > p.tpt ? JOB_WIDE : 0);
-    put(JobSum{jobs.count + k, jobs.cost + (int64_t)k * OV_NARROW}, j);
+    put(Sum{(Int)(jobs.count + k), jobs.cost + (Int)k * OV_NARROW, 0}, j);
   }
   __syncthreads();   // the jobs
-  // (with more jobs than room the rest has no work: the last one's end is the total)
-  const int J = (int)min(jobs.count + pads, (int64_t)p.cap);
+  const bool room = (int64_t)jobs.count + pads <= p.cap;
+  const int J = room ? (int)jobs.count + pads : 0;
   auto job_at = [&](int j) { return j < PLAN_JOBS ? s_job[j] : p.jobs[j]; };
   auto cost_at = [&](int j) { return j < PLAN_JOBS ? s_job[j].cost : p.jobs[j].cost; };
   int64_t all = 0;
@@ -434,6 +458,7 @@ __device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p,
         cut.ntok = j.ntok;
         if (cut.first < cut.last) {   // (else whole in one CTA)
           const int at = atomicAdd(&ps.cuts, 1);
+          atomicMax(&ps.cut_rows, j.ntok * p.ratio);
           if (writer) p.cut[at] = cut;
         }
       }
@@ -450,16 +475,12 @@ __device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p,
     }
   }
   __syncthreads();
-  if (tid == 0) {
-    const KvHead h{all, per, J, prefix_jobs, ps.cuts, 0};
-    if (writer) *p.head = h;
-    if (!all_ctas) *own_head = h;
-  }
+  if (writer && tid == 0) *p.head = KvHead{all, per, J, room ? prefix_jobs : 0, room ? (int)jobs.rows : 0, ps.cuts, ps.cut_rows, 0};
 }
 
 __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, int n_kv_heads) {
   extern __shared__ __align__(16) unsigned char psm[];
-  make_plan(b, p, n_kv_heads, *reinterpret_cast<PlanSmem*>(psm), true, nullptr, nullptr);
+  make_plan<int64_t>(b, p, n_kv_heads, *reinterpret_cast<PlanSmem*>(psm), true, nullptr);
 }
 
 // ------------------------------------------------------------------ PTX
@@ -674,15 +695,6 @@ __device__ __forceinline__ Parts parts_of(const KvJob& j, int head, int n_kv_hea
   return r;
 }
 
-__device__ __forceinline__ KvJob job_from_l2(const KvJob* j) {
-  KvJob r;
-  const int4* s = reinterpret_cast<const int4*>(j);
-  int4* d = reinterpret_cast<int4*>(&r);
-#pragma unroll
-  for (int k = 0; k < 3; k++) d[k] = __ldcg(s + k);
-  return r;
-}
-
 // One row (token, head) from its parts: x's (row rx of the 256 if cut, else at
 // home), then y's.  A lane takes the log sum of a part, the warp their largest
 // and the weights, and the rows of several parts are on their way at once.
@@ -696,7 +708,7 @@ __device__ __forceinline__ void join_row(const KvAttendArgs& a, const KvPlan& p,
 #pragma unroll
   for (int e = 0; e < E; e++) o[e] = 0.0f;
   for (int base = 0; base < count; base += 32) {
-    const int k = base + lane;
+    const int k = base + lane, here = min(32, count - base);
     const float* src = nullptr;
     float s = -INFINITY;
     if (k < count) {
@@ -705,43 +717,47 @@ __device__ __forceinline__ void join_row(const KvAttendArgs& a, const KvPlan& p,
       const bool whole = q.last < q.first;
       const int64_t at = whole ? (k < x.count ? 0 : all) + home
                                : ((int64_t)c * 2 + (c == q.c0 ? 1 : 0)) * 256 + (k < x.count ? rx : ry);
-      s = __ldcg((whole ? p.home_lse : p.part_lse) + at);
+      s = (whole ? p.home_lse : p.part_lse)[at];
       src = (whole ? p.home : p.part) + at * D;
     }
-    float big = s;
-#pragma unroll
-    for (int z = 16; z; z >>= 1) big = fmaxf(big, __shfl_xor_sync(~0u, big, z));
-    const float m2 = fmaxf(m, big);
-    const float wt = s == -INFINITY ? 0.0f : ex2(__fsub_rn(s, m2));
-    const float f = m == -INFINITY ? 0.0f : ex2(__fsub_rn(m, m2));
-    float sum = wt;
-#pragma unroll
-    for (int z = 16; z; z >>= 1) sum = __fadd_rn(sum, __shfl_xor_sync(~0u, sum, z));
-    l = fmaf(l, f, sum);
-#pragma unroll
-    for (int e = 0; e < E; e++) o[e] = __fmul_rn(o[e], f);
-    m = m2;
-    const int here = min(32, count - base);
+    float wt = 0.0f;
     for (int q = 0; q < here; q += 8) {
-      float w8[8], v[8][E];
+      float v[8][E];
 #pragma unroll
       for (int z = 0; z < 8; z++) {   // (past the last part: weight 0, the last one's row)
         const int from = min(q + z, here - 1);
-        const float w = __shfl_sync(~0u, wt, from);
-        w8[z] = q + z < here ? w : 0.0f;
         const float* r = reinterpret_cast<const float*>(__shfl_sync(~0u, reinterpret_cast<unsigned long long>(src), from)) + lane * E;
         if constexpr (E == 4) {
-          const float4 t = __ldcg(reinterpret_cast<const float4*>(r));
+          const float4 t = *reinterpret_cast<const float4*>(r);
           v[z][0] = t.x; v[z][1] = t.y; v[z][2] = t.z; v[z][3] = t.w;
         } else {
-          const float2 t = __ldcg(reinterpret_cast<const float2*>(r));
+          const float2 t = *reinterpret_cast<const float2*>(r);
           v[z][0] = t.x; v[z][1] = t.y;
         }
       }
+      if (q == 0) {   // the weights, with the first rows on their way
+        float big = s;
 #pragma unroll
-      for (int z = 0; z < 8; z++)
+        for (int z = 16; z; z >>= 1) big = fmaxf(big, __shfl_xor_sync(~0u, big, z));
+        const float m2 = fmaxf(m, big);
+        const float f = m == -INFINITY ? 0.0f : ex2(__fsub_rn(m, m2));
+        wt = s == -INFINITY ? 0.0f : ex2(__fsub_rn(s, m2));
+        float sum = wt;
 #pragma unroll
-        for (int e = 0; e < E; e++) o[e] = w8[z] == 0.0f ? o[e] : fmaf(w8[z], v[z][e], o[e]);
+        for (int z = 16; z; z >>= 1) sum = __fadd_rn(sum, __shfl_xor_sync(~0u, sum, z));
+        l = fmaf(l, f, sum);
+#pragma unroll
+        for (int e = 0; e < E; e++) o[e] = __fmul_rn(o[e], f);
+        m = m2;
+      }
+#pragma unroll
+      for (int z = 0; z < 8; z++) {
+        const float w = __shfl_sync(~0u, wt, min(q + z, here - 1));
+        if (q + z < here && w != 0.0f) {
+#pragma unroll
+          for (int e = 0; e < E; e++) o[e] = fmaf(w, v[z][e], o[e]);
+        }
+      }
     }
   }
   const float inv = l == 0.0f ? 0.0f : __fdiv_rn(1.0f, l);
@@ -758,29 +774,49 @@ __device__ __forceinline__ void join_row(const KvAttendArgs& a, const KvPlan& p,
 // Rows that have parts, a warp a row: of the jobs that a share's end cut, and of
 // shared groups, whose rows have a prefix job and an own one.  The parts' order
 // is the keys', so the result does not depend on when they came.
+// Bound: latency (plan, lengths, jobs and parts depend on each other).
 template <int D, bool HALF>
-__device__ __forceinline__ void join_rows(const KvAttendArgs& a, const KvPlan& p, const KvHead& hd, int first, int step) {
-  const int lane = threadIdx.x & 31;
+__global__ void __launch_bounds__(256) k_kv_join(const __grid_constant__ KvAttendArgs a,
+                                                 const __grid_constant__ KvPlan p) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int lane = threadIdx.x & 31, first = blockIdx.x * 8 + (threadIdx.x >> 5), step = gridDim.x * 8;
   const int hk = a.c.n_kv_heads, w2 = 2 * p.tpt, n = a.b.n_req;
-  const int64_t cuts = (int64_t)hd.cuts * 256, rows = cuts + (int64_t)hd.prefix_jobs * hk * 256;
+  const KvHead hd = *p.head;
+  auto part_row = [&](int tok, int hl) {   // a token's and head's of a job's 256
+    return (tok >= p.tpt ? 128 + (tok - p.tpt) * p.ratio : tok * p.ratio) + hl;
+  };
+  const int64_t cuts = (int64_t)hd.cuts * hd.cut_rows, rows = cuts + (int64_t)hd.shared * a.n_heads;
+  // the first prefix jobs' tokens before, a lane each
+  const int64_t before = lane < hd.prefix_jobs ? p.jobs[lane].rows : LLONG_MAX;
   for (int64_t x = first; x < rows; x += step) {
-    const int rr = (int)(x & 255), r = rr & 127, tl = r / p.ratio, hl = r - tl * p.ratio;   // of a job's 256
-    const int tok = (rr >> 7) * p.tpt + tl;
     Parts pre{0, 0, 0, 0}, own{0, 0, 0, 0};
-    int row, hq, ro = 0;
+    int row, hq, rp, ro = 0;
     if (x < cuts) {
-      const int4* c = reinterpret_cast<const int4*>(p.cut + (x >> 8));
-      const int4 c0 = __ldcg(c), c1 = __ldcg(c + 1);
-      if (tl >= p.tpt || tok >= c0.y) continue;
-      pre = Parts{c0.w, c1.x, c1.y, c1.y - c1.x + 1};
-      row = c0.x + tok;
-      hq = c0.z * p.ratio + hl;
+      const int u = (int)(x / hd.cut_rows), r = (int)(x - (int64_t)u * hd.cut_rows), tok = r / p.ratio, hl = r - tok * p.ratio;
+      const KvCut c = p.cut[u];
+      if (tok >= c.ntok) continue;
+      pre = Parts{c.c0, c.first, c.last, c.last - c.first + 1};
+      row = c.tok0 + tok;
+      hq = c.head * p.ratio + hl;
+      rp = part_row(tok, hl);
     } else {
-      const int u = (int)((x - cuts) >> 8), pj = u / hk, kh = u - pj * hk;
-      const KvJob j = job_from_l2(p.jobs + pj);
-      if (tl >= p.tpt || tok >= j.ntok) continue;
+      const int64_t t = (x - cuts) / a.n_heads;
+      hq = (int)(x - cuts - t * a.n_heads);
+      int pj;
+      if (hd.prefix_jobs <= 32) {
+        pj = __popc(__ballot_sync(~0u, before <= t)) - 1;
+      } else {
+        int lo = 0, hi = hd.prefix_jobs;
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (p.jobs[mid].rows <= t) lo = mid; else hi = mid;
+        }
+        pj = lo;
+      }
+      const KvJob j = p.jobs[pj];
+      const int tok = (int)(t - j.rows), kh = hq / p.ratio, hl = hq - kh * p.ratio;
       row = j.tok0 + tok;
-      hq = kh * p.ratio + hl;
+      rp = part_row(tok, hl);
       int i = row;   // single tokens: request i has row i
       if (!(row < n && a.b.q_start[row] == row && a.b.q_start[row + 1] == row + 1)) {
         int lo = 0, hi = n;
@@ -790,24 +826,17 @@ __device__ __forceinline__ void join_rows(const KvAttendArgs& a, const KvPlan& p
         }
         i = lo;
       }
-      const int j0 = __ldcg(p.job0 + i), q0 = a.b.q_start[i];
+      const int j0 = p.job0[i], q0 = a.b.q_start[i];
       if (j0 >= 0 && q0 >= 0 && row >= q0) {
-        const KvJob o = job_from_l2(p.jobs + min(j0 + (row - q0) / w2, hd.jobs - 1));
-        const int t = row - o.tok0;
-        if (t >= 0 && t < o.ntok) own = parts_of(o, kh, hk, hd);
-        ro = (t >= p.tpt ? 128 + (t - p.tpt) * p.ratio : t * p.ratio) + hl;
+        const KvJob o = p.jobs[min(j0 + (row - q0) / w2, hd.jobs - 1)];
+        const int ot = row - o.tok0;
+        if (ot >= 0 && ot < o.ntok) own = parts_of(o, kh, hk, hd);
+        ro = part_row(ot, hl);
       }
       pre = parts_of(j, kh, hk, hd);
     }
-    join_row<D, HALF>(a, p, pre, rr, own, ro, row, hq, lane);
+    join_row<D, HALF>(a, p, pre, rp, own, ro, row, hq, lane);
   }
-}
-
-template <int D, bool HALF>
-__global__ void __launch_bounds__(256) k_kv_join(const __grid_constant__ KvAttendArgs a,
-                                                 const __grid_constant__ KvPlan p) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  join_rows<D, HALF>(a, p, *p.head, (int)blockIdx.x * 8 + (int)(threadIdx.x >> 5), (int)gridDim.x * 8);
 }
 
 // ------------------------------------------------------------------ the kernel
@@ -920,8 +949,8 @@ struct Lay {
   static constexpr int NBAR = 2 * NST + 13 + 2 * NR;
   static constexpr int ML = MISC + 384;           // float2 [128]
   static constexpr int RUNS = ML + 1024;          // Run [NR]
-  static constexpr int START = RUNS + NR * (int)sizeof(Run);   // KvStart, KvHead
-  static constexpr int SMEM = START + (int)sizeof(KvStart) + (int)sizeof(KvHead);
+  static constexpr int START = RUNS + NR * (int)sizeof(Run);   // KvStart
+  static constexpr int SMEM = START + (int)sizeof(KvStart);
   static_assert((int)sizeof(PlanSmem) <= MISC, "the plan's memory is the tiles'");
 };
 
@@ -957,7 +986,6 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
                  MEET = QFULL + 96, RFULL = QFULL + 104, REMPTY = RFULL + 8 * NR;
   Run* const runs = reinterpret_cast<Run*>(sm + L::RUNS);
   KvStart* const start = reinterpret_cast<KvStart*>(sm + L::START);
-  KvHead* const head = reinterpret_cast<KvHead*>(sm + L::START + sizeof(KvStart));
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(sm + L::MISC + 8 * L::NBAR);
   volatile int* lost = reinterpret_cast<volatile int*>(sm + L::MISC + 8 * L::NBAR + 4);
   static_assert(8 * L::NBAR + 8 <= 384, "barriers");
@@ -990,14 +1018,10 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
   __syncthreads();
   tc_after();
   const uint32_t tmem = *s_tmem;
-  const unsigned generation = *reinterpret_cast<volatile unsigned*>(&p.meet[1]);   // (nobody moves it before this CTA has arrived)
   if (p.planned) {
-    if (tid == 0) {
-      *start = p.start[blockIdx.x];
-      *head = *p.head;
-    }
+    if (tid == 0) *start = p.start[blockIdx.x];
   } else {
-    make_plan(a.b, p, a.c.n_kv_heads, *reinterpret_cast<PlanSmem*>(sm), false, start, head);
+    make_plan<int32_t>(a.b, p, a.c.n_kv_heads, *reinterpret_cast<PlanSmem*>(sm), false, start);
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (copies into the same memory follow)
   }
   __syncthreads();
@@ -1427,29 +1451,6 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
     }
     __syncthreads();
     if (*lost) drain();
-    const KvHead hd = *head;
-    if (p.join_here && (hd.cuts > 0 || hd.prefix_jobs > 0)) {
-      // every CTA's parts are there when all have met (they all run at once: a cooperative launch)
-      if (tid == 0) {
-        __threadfence();
-        if (atomicAdd(&p.meet[0], 1u) == gridDim.x - 1) {
-          p.meet[0] = 0;
-          __threadfence();
-          atomicAdd(&p.meet[1], 1u);
-        } else {
-          const long long t = clock64();
-          while (*reinterpret_cast<volatile unsigned*>(&p.meet[1]) == generation) {
-            if (clock64() - t > (1ll << 37)) {   // (a minute)
-              *reinterpret_cast<volatile int32_t*>(p.err) = 1;
-              break;
-            }
-          }
-        }
-        __threadfence();
-      }
-      asm volatile("bar.sync 1, 256;" ::: "memory");
-      join_rows<D, HALF>(a, p, hd, (int)blockIdx.x + warp * (int)gridDim.x, (int)gridDim.x * 8);
-    }
   }
 }
 
@@ -1497,7 +1498,6 @@ size_t carve(const KvAttendArgs& a, int ctas, unsigned char* ws, KvPlan& p) {
     if (ws) ptr = reinterpret_cast<std::remove_reference_t<decltype(ptr)>>(ws + o);
     o = up(o + count * sizeof(*ptr));
   };
-  take(p.meet, 2);   // (first: in its place whatever the call's sizes)
   take(p.head, 1);
   take(p.jobs, (size_t)p.cap + 1);
   take(p.job0, n);
@@ -1511,8 +1511,6 @@ size_t carve(const KvAttendArgs& a, int ctas, unsigned char* ws, KvPlan& p) {
   take(p.home_lse, G ? 2 * rows : 0);
   return o;
 }
-
-constexpr int64_t JOIN_HERE = 2048;   // rows up to which the attention kernel joins parts itself
 
 template <int D, bool HALF>
 cudaError_t run(const KvAttendArgs& a, const KvPlan& p, const CUtensorMap* m, cudaStream_t st) {
@@ -1532,22 +1530,19 @@ cudaError_t run(const KvAttendArgs& a, const KvPlan& p, const CUtensorMap* m, cu
   c.blockDim = dim3(NT_ATT);
   c.dynamicSmemBytes = L::SMEM;
   c.stream = st;
-  cudaLaunchAttribute at;
-  c.attrs = &at;
-  c.numAttrs = p.join_here ? 1 : 0;
-  at.id = cudaLaunchAttributeCooperative;   // (its CTAs wait for one another before they join parts)
-  at.val.cooperative = 1;
   e = cudaLaunchKernelEx(&c, k, m[0], m[1], m[2], m[3], a, p);
-  if (e != cudaSuccess || p.join_here) return e;
+  if (e != cudaSuccess) return e;
   // a warp a row, no more than the GPU holds at once
-  const int64_t jobs = a.b.n_groups ? std::min<int64_t>(a.b.n_tokens / (2 * p.tpt) + a.b.n_groups, p.cap) : 0;
-  const int64_t rows = (p.ctas + jobs * a.c.n_kv_heads) * 256;
+  const int64_t rows = std::min<int64_t>((int64_t)p.ctas * 256, (int64_t)a.b.n_tokens * a.n_heads) +
+                       (a.b.n_groups ? (int64_t)a.b.n_tokens * a.n_heads : 0);
   c.gridDim = dim3((unsigned)std::min<int64_t>((rows + 7) / 8, (int64_t)p.ctas * 8));
   c.blockDim = dim3(256);
   c.dynamicSmemBytes = 0;
-  c.numAttrs = 1;
+  cudaLaunchAttribute at;   // (it is on its way while the attention kernel ends)
   at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at.val.programmaticStreamSerializationAllowed = 1;
+  c.attrs = &at;
+  c.numAttrs = 1;
   return cudaLaunchKernelEx(&c, k_kv_join<D, HALF>, a, p);
 }
 
@@ -1577,8 +1572,8 @@ cudaError_t launch_kv_attend(const KvAttendArgs& a, void* ws, int32_t* err, int 
     return cudaErrorInvalidValue;
   // up to PLAN_JOBS jobs every CTA finds its share by itself, in the time that a kernel before it and its start would
   // take; more are one CTA's work for all
-  p.planned = p.cap > PLAN_JOBS || a.b.n_groups > PLAN_GROUPS;
-  p.join_here = (int64_t)a.b.n_tokens * a.n_heads <= JOIN_HERE;
+  p.planned = p.cap > PLAN_JOBS || a.b.n_groups > PLAN_GROUPS ||
+              (int64_t)p.cap * ((a.b.max_blocks / (TK / 16) + 1) * W_WIDE + OV_WIDE) > INT_MAX;   // (costs in 32 bits)
   if (p.planned) {
     cudaError_t e = cudaFuncSetAttribute(k_kv_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(PlanSmem));
     if (e != cudaSuccess) return e;
