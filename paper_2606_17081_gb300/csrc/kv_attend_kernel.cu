@@ -580,6 +580,13 @@ __device__ __forceinline__ void tm_st32(uint32_t addr, const uint32_t* v) {
 __device__ __forceinline__ void tm_wait_ld(uint32_t* v) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" : U8(v, 0), U8(v, 8), U8(v, 16), U8(v, 24)::"memory");
 }
+// 16 lanes by 32 columns, 8 columns a group of four registers: thread t has columns
+// 2 (t % 4) and the next of rows t / 4 (registers 0, 1) and t / 4 + 8 (2, 3).
+__device__ __forceinline__ void tm_ld16(uint32_t* v, uint32_t addr) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : W8(v, 0), W8(v, 8) : "r"(addr));
+}
 __device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ float ex2(float x) {
@@ -1402,6 +1409,63 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
           if (!direct) (whole ? p.home_lse : p.part_lse)[at] = lse2;
           else if (a.lse) a.lse[(int64_t)row * a.n_heads + hq] = __fmul_rn(lse2, 0.6931471805599453f);
         }
+        const unsigned lives = __ballot_sync(~0u, live);
+        if (!split && __popc(lives) > 8) {
+          // many rows: 16 at a time, four threads to a row, 64 bytes a store (a thread a row would touch as many
+          // lines as there are rows with every store)
+          char* const dst = direct ? reinterpret_cast<char*>(out) : reinterpret_cast<char*>(part);
+          const int q = lane & 3;
+#pragma unroll 1
+          for (int h = 0; h < 32; h += 16) {
+            const int ra = h + (lane >> 2), rb = ra + 8;
+            uint32_t v[D / 2];
+#pragma unroll
+            for (int c = 0; c < D; c += 32) tm_ld16(v + c / 2, tmem + lanes + ((uint32_t)h << 16) + 256 + s * D + c);
+            const float fa = __shfl_sync(~0u, f0, ra), fb = __shfl_sync(~0u, f0, rb);
+            char* const da = reinterpret_cast<char*>(__shfl_sync(~0u, reinterpret_cast<unsigned long long>(dst), ra));
+            char* const db = reinterpret_cast<char*>(__shfl_sync(~0u, reinterpret_cast<unsigned long long>(dst), rb));
+            const bool la = (lives >> ra) & 1, lb = (lives >> rb) & 1;
+#pragma unroll
+            for (int c = 0; c < D / 2; c += 32) tm_wait_ld(v + c);
+#pragma unroll
+            for (int c = 0; c < D; c += 32) {
+              uint32_t* o = v + c / 2;
+#pragma unroll
+              for (int k = 0; k < 16; k++) o[k] = __float_as_uint(__fmul_rn(__uint_as_float(o[k]), k & 2 ? fb : fa));
+              if (direct) {
+                // of each row a thread has two columns of each group; it gets the eight of group q
+#pragma unroll
+                for (int z = 0; z < 4; z += 2) {
+                  uint32_t w[4];
+#pragma unroll
+                  for (int k = 0; k < 4; k++) w[k] = pack2<HALF>(__uint_as_float(o[4 * k + z]), __uint_as_float(o[4 * k + z + 1]));
+#pragma unroll
+                  for (int k = 0; k < 4; k += 2) {   // threads 1 apart
+                    const uint32_t y = __shfl_xor_sync(~0u, q & 1 ? w[k] : w[k + 1], 1);
+                    if (q & 1) w[k] = y; else w[k + 1] = y;
+                  }
+#pragma unroll
+                  for (int k = 0; k < 2; k++) {      // and 2 apart
+                    const uint32_t y = __shfl_xor_sync(~0u, q & 2 ? w[k] : w[k + 2], 2);
+                    if (q & 2) w[k] = y; else w[k + 2] = y;
+                  }
+                  if (z ? lb : la) *reinterpret_cast<uint4*>((z ? db : da) + (c + 8 * q) * 2) = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+              } else {
+                // it gets four columns of group k or, the odd ones, of the next
+#pragma unroll
+                for (int z = 0; z < 4; z += 2)
+#pragma unroll
+                  for (int k = 0; k < 4; k += 2) {
+                    uint32_t* u = o + 4 * k + z;   // u[0], u[1]: group k, u[4], u[5]: the next
+                    const uint32_t y0 = __shfl_xor_sync(~0u, q & 1 ? u[0] : u[4], 1), y1 = __shfl_xor_sync(~0u, q & 1 ? u[1] : u[5], 1);
+                    const uint4 w = q & 1 ? make_uint4(y0, y1, u[4], u[5]) : make_uint4(u[0], u[1], y0, y1);
+                    if (z ? lb : la) *reinterpret_cast<uint4*>((z ? db : da) + (c + 8 * (k + (q & 1)) + 4 * (q >> 1)) * 4) = w;
+                  }
+              }
+            }
+          }
+        } else {
 #pragma unroll 1
         for (int c = 0; c < D; c += 64) {
           uint32_t o[64];
@@ -1438,6 +1502,7 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
                 *reinterpret_cast<float4*>(part + c + k) = make_float4(y[k], y[k + 1], y[k + 2], y[k + 3]);
             }
           }
+        }
         }
       }
       tc_before();
