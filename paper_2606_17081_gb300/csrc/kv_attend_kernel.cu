@@ -31,7 +31,7 @@ namespace {
 constexpr int TK = 128;        // keys of a tile
 // Costs: a tile of a job of at most 128 rows, one of a larger job, and a job's
 // own (its rows' loads and stores).
-constexpr int W_NARROW = 4, W_WIDE = 6, OV_NARROW = 3, OV_WIDE = 10;
+constexpr int W_NARROW = 4, W_WIDE = 5, OV_NARROW = 3, OV_WIDE = 10;
 constexpr int NT_PLAN = 1024;
 constexpr int NT_ATT = 384;
 constexpr int PLAN_GROUPS = 1024;   // groups whose sums are kept in shared memory
