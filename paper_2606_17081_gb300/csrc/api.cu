@@ -1408,7 +1408,7 @@ rs_status kv_append(rs_ctx* ctx, const rs_kv_cache* cache, const void* k_dev, co
   if (n_tokens == 1) token_stride = 0;
   if (c.n_kv_heads == 1) head_stride = 0;
   if (token_stride < 0 || head_stride < 0) return fail(ctx, RS_ERR_INVALID, "negative stride");
-  CK(launch_kv_append(c, k_dev, v_dev, token_stride, head_stride, n_tokens, slots_dev, ctx->st),
+  CK(launch_kv_append(c, k_dev, v_dev, token_stride, head_stride, n_tokens, slots_dev, ctx->sms, ctx->st),
      "KV append launch");
   return RS_OK;
 }

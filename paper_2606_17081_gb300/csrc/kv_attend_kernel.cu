@@ -97,6 +97,7 @@ struct KvPlan {
   int32_t tpt;          // tokens of 128 rows
   int32_t ratio;        // heads of a kv head
   int32_t planned;      // the plan is there before the attention kernel begins
+  int32_t whole;        // no job is cut
 };
 
 namespace {
@@ -429,23 +430,39 @@ __device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p,
   }
   // two tiles at least, one for each stream of a CTA
   const int64_t per = max((all + p.ctas - 1) / p.ctas, (int64_t)(2 * W_NARROW + OV_NARROW));
+  // the job and head that has cost u < all, and how far in
+  auto locate = [&](int64_t u, KvStart& s) {
+    int lo = 0, hi = J;   // the last job that starts at or before u
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (cost_at(mid) * n_kv_heads <= u) lo = mid; else hi = mid;
+    }
+    s.job = lo;
+    s.j = job_at(lo);
+    const int64_t in = u - s.j.cost * n_kv_heads;
+    const int cj = job_cost(s.j.nt, s.j.flags);
+    s.head = (int)quotient(in, cj);
+    s.off = (int)(in - (int64_t)s.head * cj);
+  };
+  // the end of the job and head that has cost u - 1 (u <= all): shares begin and end there when none is to be cut
+  auto whole_end = [&](int64_t u) {
+    if (u <= 0) return (int64_t)0;
+    KvStart s;
+    locate(u - 1, s);
+    return u - 1 - s.off + job_cost(s.j.nt, s.j.flags);
+  };
   for (int c = tid; c < p.ctas; c += nth) {
-    const int64_t u = c * per;
+    int64_t u = c * per, end = min(u + per, all);
     KvStart s = {};
-    if (u < all) {
-      int lo = 0, hi = J;   // the last job that starts at or before u
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (cost_at(mid) * n_kv_heads <= u) lo = mid; else hi = mid;
-      }
-      const KvJob j = job_at(lo);
+    if (p.whole && u < all) {
+      u = whole_end(u);
+      end = whole_end(end);
+    }
+    if (u < end) {
+      locate(u, s);
+      s.rem = end - u;
+      const KvJob j = s.j;
       const int cj = job_cost(j.nt, j.flags);
-      const int64_t in = u - j.cost * n_kv_heads;
-      s.job = lo;
-      s.head = (int)quotient(in, cj);
-      s.off = (int)(in - (int64_t)s.head * cj);
-      s.rem = min(per, all - u);
-      s.j = j;
       const int64_t u0 = u - s.off;
       if (s.off > 0 && j.nt > 0 && (j.flags & JOB_ALONE) && u0 >= u - per) {   // not cut before
         int t0, t1, e = (int)quotient(u0 + cj - 1, per);
@@ -469,7 +486,7 @@ __device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p,
   if (!all_ctas) {
     const int64_t u = blockIdx.x * per;
     for (int j = tid; j < J; j += nth) {
-      const KvJob x = s_job[j];
+      const KvJob x = s_job[j];   // (a share without cuts begins later and ends in its last job)
       const int64_t at = x.cost * n_kv_heads;
       if (at < u + per && at + (int64_t)job_cost(x.nt, x.flags) * n_kv_heads > u) p.jobs[j] = x;
     }
@@ -480,6 +497,7 @@ __device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p,
 
 __global__ void __launch_bounds__(NT_PLAN) k_kv_plan(rs_kv_batch b, KvPlan p, int n_kv_heads) {
   extern __shared__ __align__(16) unsigned char psm[];
+  behind_stream();
   make_plan<int64_t>(b, p, n_kv_heads, *reinterpret_cast<PlanSmem*>(psm), true, nullptr);
 }
 
@@ -785,7 +803,7 @@ __device__ __forceinline__ void join_row(const KvAttendArgs& a, const KvPlan& p,
 template <int D, bool HALF>
 __global__ void __launch_bounds__(256) k_kv_join(const __grid_constant__ KvAttendArgs a,
                                                  const __grid_constant__ KvPlan p) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  behind_stream();
   const int lane = threadIdx.x & 31, first = blockIdx.x * 8 + (threadIdx.x >> 5), step = gridDim.x * 8;
   const int hk = a.c.n_kv_heads, w2 = 2 * p.tpt, n = a.b.n_req;
   const KvHead hd = *p.head;
@@ -1025,6 +1043,7 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
   __syncthreads();
   tc_after();
   const uint32_t tmem = *s_tmem;
+  behind_stream();
   if (p.planned) {
     if (tid == 0) *start = p.start[blockIdx.x];
   } else {
@@ -1032,7 +1051,6 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (copies into the same memory follow)
   }
   __syncthreads();
-  asm volatile("griddepcontrol.launch_dependents;");
 
   auto drain = [] {   // copies in flight end before the CTA's memory is another's
     const long long t = clock64();
@@ -1590,25 +1608,12 @@ cudaError_t run(const KvAttendArgs& a, const KvPlan& p, const CUtensorMap* m, cu
     return cudaFuncGetAttributes(&f, k_kv_attend<D, HALF>) == cudaSuccess ? f.numRegs : 0;
   }();
   if (regs * 3 < 2 * 208 + 88) return cudaErrorInvalidKernelImage;
-  cudaLaunchConfig_t c = {};
-  c.gridDim = dim3(p.ctas);
-  c.blockDim = dim3(NT_ATT);
-  c.dynamicSmemBytes = L::SMEM;
-  c.stream = st;
-  e = cudaLaunchKernelEx(&c, k, m[0], m[1], m[2], m[3], a, p);
-  if (e != cudaSuccess) return e;
+  e = launch_behind(k, p.ctas, NT_ATT, L::SMEM, st, m[0], m[1], m[2], m[3], a, p);
+  if (e != cudaSuccess || p.whole) return e;
   // a warp a row, no more than the GPU holds at once
   const int64_t rows = std::min<int64_t>((int64_t)p.ctas * 256, (int64_t)a.b.n_tokens * a.n_heads) +
                        (a.b.n_groups ? (int64_t)a.b.n_tokens * a.n_heads : 0);
-  c.gridDim = dim3((unsigned)std::min<int64_t>((rows + 7) / 8, (int64_t)p.ctas * 8));
-  c.blockDim = dim3(256);
-  c.dynamicSmemBytes = 0;
-  cudaLaunchAttribute at;   // (it is on its way while the attention kernel ends)
-  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at.val.programmaticStreamSerializationAllowed = 1;
-  c.attrs = &at;
-  c.numAttrs = 1;
-  return cudaLaunchKernelEx(&c, k_kv_join<D, HALF>, a, p);
+  return launch_behind(k_kv_join<D, HALF>, (unsigned)std::min<int64_t>((rows + 7) / 8, (int64_t)p.ctas * 8), 256, 0, st, a, p);
 }
 
 }  // namespace
@@ -1635,6 +1640,10 @@ cudaError_t launch_kv_attend(const KvAttendArgs& a, void* ws, int32_t* err, int 
   if (!encode(&m[0], half, a.c.k, 4, ks, kst, kbox) || !encode(&m[1], half, a.c.v, 4, ks, kst, kbox) ||
       !encode(&m[2], half, a.q, 3, qs, qst, qbox) || !encode(&m[3], half, a.q, 3, qs, qst, qbox1))
     return cudaErrorInvalidValue;
+  // without prefixes to join and with rows of at most 16 blocks a job is two tiles, one for each stream of a CTA: none is
+  // cut, and nothing is left to a second launch (one token over 6 keys: 14.2 us a call against 17.8 us; at 64 blocks the
+  // tiles one after the other cost as much as the launch)
+  p.whole = a.b.n_groups == 0 && a.b.max_blocks <= 2 * TK / 16;
   // up to PLAN_JOBS jobs every CTA finds its share by itself, in the time that a kernel before it and its start would
   // take; more are one CTA's work for all
   p.planned = p.cap > PLAN_JOBS || a.b.n_groups > PLAN_GROUPS ||
@@ -1642,8 +1651,7 @@ cudaError_t launch_kv_attend(const KvAttendArgs& a, void* ws, int32_t* err, int 
   if (p.planned) {
     cudaError_t e = cudaFuncSetAttribute(k_kv_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(PlanSmem));
     if (e != cudaSuccess) return e;
-    k_kv_plan<<<1, NT_PLAN, sizeof(PlanSmem), st>>>(a.b, p, a.c.n_kv_heads);
-    e = cudaGetLastError();
+    e = launch_behind(k_kv_plan, 1, NT_PLAN, sizeof(PlanSmem), st, a.b, p, (int)a.c.n_kv_heads);
     if (e != cudaSuccess) return e;
   }
   if (D == 128) return half ? run<128, true>(a, p, m, st) : run<128, false>(a, p, m, st);

@@ -275,13 +275,36 @@ cudaError_t launch_route_release(const RouterState& s, const int32_t* worker, co
 cudaError_t launch_clear_tables(uint64_t* keys, uint32_t* stamp, size_t nslots, CacheMeta* meta,
                                 size_t nmeta, cudaStream_t st);
 
-// A worker's paged KV cache (arguments checked by the caller).
+// A worker's paged KV cache (arguments checked by the caller).  These kernels
+// follow one another in a step, so each may begin before the one ahead of it in
+// the stream has ended: it waits (behind_stream) before it touches memory, and it
+// lets the next begin at once.
+#ifdef __CUDACC__
+__device__ __forceinline__ void behind_stream() {
+  asm volatile("griddepcontrol.launch_dependents;");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+template <class Kernel, class... Args>
+cudaError_t launch_behind(Kernel k, unsigned grid, unsigned threads, size_t smem, cudaStream_t st, const Args&... args) {
+  cudaLaunchConfig_t c = {};
+  c.gridDim = dim3(grid);
+  c.blockDim = dim3(threads);
+  c.dynamicSmemBytes = smem;
+  c.stream = st;
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  c.attrs = &at;
+  c.numAttrs = 1;
+  return cudaLaunchKernelEx(&c, k, args...);
+}
+#endif
 cudaError_t launch_kv_tables(const rs_kv_batch& b, const int32_t* q_len, const int32_t* prev_len,
                              const int32_t* prefix_blocks, int64_t prefix_stride,
                              const int32_t* free_ids, int64_t n_free, int32_t* positions,
                              int64_t* slots, int64_t* counts, int sms, cudaStream_t st);
 cudaError_t launch_kv_append(const rs_kv_cache& c, const void* k, const void* v, int64_t ts, int64_t hs,
-                             int n_tokens, const int64_t* slots, cudaStream_t st);
+                             int n_tokens, const int64_t* slots, int sms, cudaStream_t st);
 struct KvAttendArgs {
   rs_kv_cache c;
   rs_kv_batch b;
