@@ -140,6 +140,47 @@ def test_scores_that_grow_along_the_keys(ctx, growth, heads, new):
     compare(s, *attend(ctx, s))
 
 
+@pytest.mark.parametrize("growth", [1.0, 40.0, -40.0])
+def test_scores_that_grow_in_fp16(ctx, growth):
+    """Weights stay within fp16's range although the running maximum starts far below."""
+    n = 700
+    s = Step(18, [1, 90], [n - 1, n - 90], 4, 2, 64, HF)
+    for i in range(2):
+        for j in range(n):
+            s.k[int(s.table[i, j // BLOCK]), :, j % BLOCK, 0] = growth * j / n
+    s.q[:, :, 0] = 6.0
+    s.q[:, :, 1:] *= 0.25
+    compare(s, *attend(ctx, s))
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", [(8, 2, 128), (16, 16, 64), (5, 1, 64)])
+def test_short_tables_are_not_cut(ctx, heads, kv_heads, dim):
+    """Rows of at most 16 blocks and no groups: the jobs stay whole."""
+    r = random.Random(dim)
+    new = [r.choice([0, 1, 1, 3, 40]) for _ in range(70)]
+    s = Step(16, new, [r.randint(0, 200) for _ in new], heads, kv_heads, dim, BF, pad=5)
+    assert s.table.shape[1] <= 16
+    compare(s, *attend(ctx, s))
+
+
+def test_many_requests_and_groups(ctx):
+    """More requests, and more groups, than a CTA plans for itself; more prefix jobs than a warp has lanes."""
+    r = random.Random(17)
+    for n, per, prefix in ((1100, 0, 0), (1200, 1, 32), (90, 2, 400), (1030, 10, 160)):
+        starts = list(range(0, n, per)) + [n] if per else None
+        new = [r.choice([0, 1, 1, 1, 2]) for _ in range(n)]
+        ctxs = [prefix + r.randint(0, 40) for _ in range(n)]
+        s = Step(17, new, ctxs, 2, 1, 64, BF, starts, [prefix] * (len(starts) - 1) if per else None, pad=1)
+        compare(s, *attend(ctx, s))
+
+
+def test_a_long_prompt_beside_single_tokens(ctx):
+    """More jobs than a CTA plans for itself, with a group's prefix among them."""
+    ctxs = [256] * 40 + [300]
+    s = Step(19, [1] * 40 + [1100], ctxs, 128, 1, 64, BF, [0, 40], [256])
+    compare(s, *attend(ctx, s))
+
+
 def test_strided_and_shifted_tensors(ctx):
     """q as columns of a projection, out inside a wider buffer that stays as it was around it."""
     s = Step(9, [1, 4, 30], [50, 200, 10], 8, 2, 64, BF)
