@@ -1,19 +1,26 @@
-// Causal attention over a paged KV cache (kv_attend): k_kv_plan cuts the step
-// into jobs, k_kv_attend runs them on the tensor cores, k_kv_join joins parts.
+// Causal attention over a paged KV cache (kv_attend): a plan cuts the step into
+// jobs, k_kv_attend runs them on the tensor cores, k_kv_join joins parts.
 //
 // Mathematics.  A row (token, head) needs o = sum_j p_j v_j / sum_j p_j over
 // the keys j below its limit, p_j = exp(scale s_j), s = q K^T.  Over any part
-// of the keys the triple (m, l, o), m a bound of the scores, l = sum exp(s - m),
-// o = sum exp(s - m) v, is enough: parts join with weights exp(m_part - m).  So
-// a job walks its keys once, 128 at a time, and the keys of a row may be cut
-// anywhere: between a prefix shared by a group (a job whose rows are all the
-// group's tokens) and the requests' own keys, and between CTAs.
+// of the keys the triple (m, l, o), m a reference for the scores, l = sum
+// exp(s - m), o = sum exp(s - m) v, is enough: parts join with weights
+// exp(m_part - m).  So a job walks its keys once, 128 at a time, and the keys of
+// a row may be cut anywhere: between a prefix shared by a group (a job whose rows
+// are all the group's tokens) and the requests' own keys, and between CTAs.
 //
 // A job is up to 2 * 128 rows x one kv head x a range of keys.  Rows are
 // tokens x the heads of the kv head (so the K and V of a head are read once for
 // all of them).  The jobs' tiles are numbered through, and CTA c takes an equal
 // share of the numbers (one CTA an SM): whole jobs write out directly, jobs
-// cut by a share's end leave parts.
+// cut by a share's end leave parts in 32 bits.
+//
+// What bounds it (one GB300): single tokens over long contexts, HBM (256 requests
+// of 256 to 8192 own tokens, 8 kv heads of 128: 2.4 GB in 358 us, 6.7 TB/s); prompts
+// and prefixes that many rows share, the tensor cores (4096 tokens behind 12 288,
+// 32 heads: 620 us, 1.55 PFLOP/s, 128 keys for 256 rows in 1.3 us of which the
+// products alone take 1.05); short steps, the chain plan - loads - product - softmax -
+// product - stores - join (one token over 701 keys: 14 us).
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -29,8 +36,12 @@ namespace rs {
 namespace {
 
 constexpr int TK = 128;        // keys of a tile
-// Costs: a tile of a job of at most 128 rows, one of a larger job, and a job's
-// own (its rows' loads and stores).
+// Costs, in quarters of a microsecond or so: a tile of a job of at most 128 rows,
+// one of a larger job, and a job's own (its rows' loads and stores).  A wide tile
+// takes 1.3 us, a narrow one 0.8 us from L2 and 1.4 us where all SMs wait for HBM.
+// 64 requests on a prefix of 32 768, 8 groups of 256 in all, 6 prompts of 100 to
+// 2047 on a prefix: 83, 427, 259 us; with 4, 6, 3, 10: 86, 427, 273 us; with equal
+// tiles and OV 2 for all: 142, 524, 299 us (on an earlier kernel).
 constexpr int W_NARROW = 4, W_WIDE = 5, OV_NARROW = 3, OV_WIDE = 10;
 constexpr int NT_PLAN = 1024;
 constexpr int NT_ATT = 384;
@@ -192,11 +203,12 @@ struct PlanSmem {
 // once at up to a request a thread, group sums and jobs live in shared memory at
 // ordinary sizes.  Starts that decrease can ask for more jobs than there is room
 // for: then there is no work at all.
-//   all = true: one CTA for everybody, starts into p.start.
-//   all = false (at most PLAN_JOBS jobs and PLAN_GROUPS groups): every CTA for
-//     itself, its start into *mine and the jobs of its share into p.jobs; what the
-//     joining needs is written by CTA 0.
-// Int: wide enough for all jobs' cost.
+//   all_ctas: one CTA for everybody, starts into p.start.
+//   else (at most PLAN_JOBS jobs and PLAN_GROUPS groups): every CTA for itself, its
+//     start into *own_start and the jobs of its share into p.jobs; what the joining
+//     needs is written by CTA 0.  3 us for one request, 5 us for 64 in groups; as a
+//     kernel of its own before the attention kernel's start it cost 4 us more.
+// Int: wide enough for all jobs' cost (64-bit sums made the plan 1 us longer).
 template <class Int>
 __device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p, int n_kv_heads, PlanSmem& ps, bool all_ctas,
                                           KvStart* own_start) {
@@ -799,7 +811,10 @@ __device__ __forceinline__ void join_row(const KvAttendArgs& a, const KvPlan& p,
 // Rows that have parts, a warp a row: of the jobs that a share's end cut, and of
 // shared groups, whose rows have a prefix job and an own one.  The parts' order
 // is the keys', so the result does not depend on when they came.
-// Bound: latency (plan, lengths, jobs and parts depend on each other).
+// Bound: latency (plan, lengths, jobs and parts depend on each other): 2 us for
+// the rows of one token, 5 to 8 us for the shared rows of 16 to 256.  Joining in the
+// attention kernel, behind a barrier of all CTAs, took as long and left fewer warps
+// to it (16 rows a group on a prefix of 32 768: 49 us in all against 44 us).
 template <int D, bool HALF>
 __global__ void __launch_bounds__(256) k_kv_join(const __grid_constant__ KvAttendArgs a,
                                                  const __grid_constant__ KvPlan p) {
@@ -989,13 +1004,25 @@ __device__ __forceinline__ int vplace(int s, int i, int n0, int n1) {
 }
 
 // Two streams of 128 rows share the tensor cores, so that one's softmax runs
-// under the other's products.  Warps 0-3 and 4-7 are the streams' softmax, a thread a row; warp 8 issues the products and
-// warp 9 the loads.
-// TMEM: S of each stream 128 columns (P, 64 columns, overwrites it), O D each.
+// under the other's products.  Warps 0-3 and 4-7 are the streams' softmax, a
+// thread a row (so no reduction crosses threads); warp 8 issues the products, warp
+// 9 the loads, warp 10 finds the runs.  Warps 8 and 9 run as one and let one
+// elected thread issue: from a divergent branch the same products took 900 us
+// instead of 650 us (4096 tokens behind 12 288).
+// Shared memory: two slots of 128 rows, the rest a ring of K and V tiles (160 KB:
+// at 43 bytes a nanosecond and SM and 1.5 us of latency HBM asks for 65 KB), each
+// loaded page by page from its block (swizzled 128-byte rows, 2 copies of 2 KB a
+// page at D = 128).
+// TMEM: S of each stream 128 columns (P, 64 columns, overwrites it), O D each:
+// full at D = 128, so a stream's next scores wait for its last weights' product.
 // The m of a row is the largest score of its first 32 keys and moves only when a
 // tile's weights sum to more than 2^15 (up to there each is in range of fp16, and
 // bf16 weights are as exact at any size), which hardly happens: O and l are
-// scaled then.
+// scaled then.  Scores, m, l and O are 32 bits; the weights are rounded once to
+// the cache's type, l sums them unrounded.
+// Measured and not kept: 32 columns of scores loaded while 32 are worked on
+// (1016 us against 900 us); the running maximum in every tile; rows written with
+// O kept in registers past its release (spills).
 template <int D, bool HALF>
 __global__ void __launch_bounds__(NT_ATT, 1)
 k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
