@@ -1667,10 +1667,10 @@ cudaError_t launch_kv_attend(const KvAttendArgs& a, void* ws, int32_t* err, int 
   if (!encode(&m[0], half, a.c.k, 4, ks, kst, kbox) || !encode(&m[1], half, a.c.v, 4, ks, kst, kbox) ||
       !encode(&m[2], half, a.q, 3, qs, qst, qbox) || !encode(&m[3], half, a.q, 3, qs, qst, qbox1))
     return cudaErrorInvalidValue;
-  // without prefixes to join and with rows of at most 16 blocks a job is two tiles, one for each stream of a CTA: none is
-  // cut, and nothing is left to a second launch (one token over 6 keys: 14.2 us a call against 17.8 us; at 64 blocks the
-  // tiles one after the other cost as much as the launch)
-  p.whole = a.b.n_groups == 0 && a.b.max_blocks <= 2 * TK / 16;
+  // Without prefixes to join and with tables of at most 64 blocks (eight tiles, four a stream of a CTA) no job is cut and
+  // nothing is left to join.  Whole and cut, us a call in a replayed graph, 32 heads on 8: one token over 255 keys 9.1 and
+  // 10.3, over 1023 12.5 and 14.2, over 1535 14.7 and 14.4; 64 tokens over 511 27.1 and 33.4, over 1023 43.3 and 46.7
+  p.whole = a.b.n_groups == 0 && a.b.max_blocks <= 64;
   // up to PLAN_JOBS jobs every CTA finds its share by itself, in the time that a kernel before it and its start would
   // take; more are one CTA's work for all
   p.planned = p.cap > PLAN_JOBS || a.b.n_groups > PLAN_GROUPS ||
