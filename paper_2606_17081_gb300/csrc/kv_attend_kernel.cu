@@ -206,7 +206,7 @@ struct PlanSmem {
 //   all_ctas: one CTA for everybody, starts into p.start.
 //   else (at most PLAN_JOBS jobs and PLAN_GROUPS groups): every CTA for itself, its
 //     start into *own_start and the jobs of its share into p.jobs; what the joining
-//     needs is written by CTA 0.  3 us for one request, 5 us for 64 in groups; as a
+//     needs is written by the last one.  3 us for one request, 5 us for 64 in groups; as a
 //     kernel of its own before the attention kernel's start it cost 4 us more.
 // Int: wide enough for all jobs' cost (64-bit sums made the plan 1 us longer).
 template <class Int>
@@ -214,7 +214,7 @@ __device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p,
                                           KvStart* own_start) {
   using Sum = JobSum<Int>;
   Sum(*scan)[32] = reinterpret_cast<Sum(*)[32]>(ps.scan);
-  const bool writer = all_ctas || blockIdx.x == 0;
+  const bool writer = all_ctas || blockIdx.x == gridDim.x - 1;   // (of a short step the last CTA has no share)
   KvJob* s_job = ps.job;
   using Acc = std::conditional_t<sizeof(Int) == 4, unsigned, unsigned long long>;
   Acc* s_sum = reinterpret_cast<Acc*>(ps.sum);
@@ -476,7 +476,7 @@ __device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p,
       const KvJob j = s.j;
       const int cj = job_cost(j.nt, j.flags);
       const int64_t u0 = u - s.off;
-      if (s.off > 0 && j.nt > 0 && (j.flags & JOB_ALONE) && u0 >= u - per) {   // not cut before
+      if (writer && s.off > 0 && j.nt > 0 && (j.flags & JOB_ALONE) && u0 >= u - per) {   // not cut before
         int t0, t1, e = (int)quotient(u0 + cj - 1, per);
         KvCut cut = {};
         cut.c0 = c - 1;
@@ -486,9 +486,8 @@ __device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p,
         cut.head = s.head;
         cut.ntok = j.ntok;
         if (cut.first < cut.last) {   // (else whole in one CTA)
-          const int at = atomicAdd(&ps.cuts, 1);
           atomicMax(&ps.cut_rows, j.ntok * p.ratio);
-          if (writer) p.cut[at] = cut;
+          p.cut[atomicAdd(&ps.cuts, 1)] = cut;
         }
       }
     }
@@ -1131,8 +1130,7 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
           auto fetch = [&](int pair) {
             const int i = 2 * pair + ((lane >> 3) & 1), t = g.t0 + (split ? 2 * i + (lane >> 4) : i);
             const int pg = p0 + t * (TK / 16);
-            int id = t < g.t1 && pg < pend ? pages[pg] : 0;
-            return id < 0 || id >= a.c.n_blocks ? (int)a.c.n_blocks : id;
+            return t < g.t1 && pg < pend ? pages[pg] : 0;   // (as it is: nothing waits for it here)
           };
           int now = r.page[lane], ahead = fetch(1), old = 0, at = 0;
           for (int u = 1; u < 4 * (max(n0, n1) + 1); u++) {
@@ -1143,7 +1141,7 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
             if ((i >> 1) > at) {
               at++;
               old = now;
-              now = ahead;
+              now = ahead < 0 || ahead >= a.c.n_blocks ? (int)a.c.n_blocks : ahead;   // (reads as zeros)
               ahead = fetch(at + 1);
             }
             const int from = (i >> 1) == at ? now : old;
