@@ -93,7 +93,7 @@ struct __align__(16) KvStart {
 struct KvPlan {
   KvHead* head;
   KvJob* jobs;          // [cap + 1]
-  int32_t* job0;        // [n_req] first own job, or -1
+  int4* shared;         // [n_tokens] of the shared groups' tokens, in order: row, prefix job, own job
   int32_t* gjob;        // [n_groups] first prefix job, -1: not shared (more than PLAN_GROUPS groups)
   unsigned long long* gsum;   // [4 n_groups] (more than PLAN_GROUPS groups)
   KvStart* start;       // [ctas]
@@ -398,7 +398,15 @@ __device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p,
     at.cost += jobs.cost;
     jobs.count += total.count;
     jobs.cost += total.cost;
-    if (writer && i < n) p.job0[i] = x.count > 0 && at.count + x.count <= p.cap ? (int32_t)at.count : -1;
+    // where its tokens' parts will be, for the join
+    auto share = [&](int t, int q0, int g, int job0) {
+      const int pj = gjob[g];
+      const KvJob& j = pj < PLAN_JOBS ? s_job[pj] : p.jobs[pj];
+      const int64_t in = q0 + t - j.tok0, to = j.rows + in;
+      if (in >= 0 && to < b.n_tokens) p.shared[to] = make_int4(q0 + t, pj + (int)(in / w2), job0 + t / w2, 0);
+    };
+    if (writer && x.count == 1 && !alone)
+      for (int t = 0; t < r.q; t++) share(t, r.q0, r.g, (int)at.count);
     if (x.count == 1) put(at, one);
     for (unsigned todo = longer; todo; todo &= todo - 1) {
       const int src = __ffs(todo) - 1;
@@ -406,6 +414,9 @@ __device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p,
       const int s0 = __shfl_sync(~0u, r.q0, src), sq = __shfl_sync(~0u, r.q, src), sk = __shfl_sync(~0u, r.kv, src);
       const int s1 = __shfl_sync(~0u, key0, src), sa = __shfl_sync(~0u, alone, src);
       Sum sat{__shfl_sync(~0u, at.count, src), __shfl_sync(~0u, at.cost, src), 0};
+      const int sg = __shfl_sync(~0u, r.g, src);
+      if (writer && !sa)
+        for (int t = lane; t < sq; t += 32) share(t, s0, sg, (int)sat.count);
       for (int k0 = 0; k0 < sc; k0 += 32) {
         const int k = k0 + lane;
         const KvJob j = job(min(k, sc - 1), si, s0, sq, sk, s1, sa);
@@ -819,14 +830,12 @@ __global__ void __launch_bounds__(256) k_kv_join(const __grid_constant__ KvAtten
                                                  const __grid_constant__ KvPlan p) {
   behind_stream();
   const int lane = threadIdx.x & 31, first = blockIdx.x * 8 + (threadIdx.x >> 5), step = gridDim.x * 8;
-  const int hk = a.c.n_kv_heads, w2 = 2 * p.tpt, n = a.b.n_req;
+  const int hk = a.c.n_kv_heads;
   const KvHead hd = *p.head;
   auto part_row = [&](int tok, int hl) {   // a token's and head's of a job's 256
     return (tok >= p.tpt ? 128 + (tok - p.tpt) * p.ratio : tok * p.ratio) + hl;
   };
   const int64_t cuts = (int64_t)hd.cuts * hd.cut_rows, rows = cuts + (int64_t)hd.shared * a.n_heads;
-  // the first prefix jobs' tokens before, a lane each
-  const int64_t before = lane < hd.prefix_jobs ? p.jobs[lane].rows : LLONG_MAX;
   for (int64_t x = first; x < rows; x += step) {
     Parts pre{0, 0, 0, 0}, own{0, 0, 0, 0};
     int row, hq, rp, ro = 0;
@@ -841,38 +850,17 @@ __global__ void __launch_bounds__(256) k_kv_join(const __grid_constant__ KvAtten
     } else {
       const int64_t t = (x - cuts) / a.n_heads;
       hq = (int)(x - cuts - t * a.n_heads);
-      int pj;
-      if (hd.prefix_jobs <= 32) {
-        pj = __popc(__ballot_sync(~0u, before <= t)) - 1;
-      } else {
-        int lo = 0, hi = hd.prefix_jobs;
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (p.jobs[mid].rows <= t) lo = mid; else hi = mid;
-        }
-        pj = lo;
-      }
-      const KvJob j = p.jobs[pj];
-      const int tok = (int)(t - j.rows), kh = hq / p.ratio, hl = hq - kh * p.ratio;
-      row = j.tok0 + tok;
+      const int4 e = p.shared[t];
+      // (starts that decrease leave entries unwritten)
+      if (e.y < 0 || e.y >= hd.prefix_jobs || e.z < 0 || e.z >= hd.jobs) continue;
+      const KvJob j = p.jobs[e.y], o = p.jobs[e.z];
+      const int kh = hq / p.ratio, hl = hq - kh * p.ratio, tok = e.x - j.tok0, ot = e.x - o.tok0;
+      if (tok < 0 || tok >= j.ntok || ot < 0 || ot >= o.ntok) continue;
+      row = e.x;
       rp = part_row(tok, hl);
-      int i = row;   // single tokens: request i has row i
-      if (!(row < n && a.b.q_start[row] == row && a.b.q_start[row + 1] == row + 1)) {
-        int lo = 0, hi = n;
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (a.b.q_start[mid] <= row) lo = mid; else hi = mid;
-        }
-        i = lo;
-      }
-      const int j0 = p.job0[i], q0 = a.b.q_start[i];
-      if (j0 >= 0 && q0 >= 0 && row >= q0) {
-        const KvJob o = p.jobs[min(j0 + (row - q0) / w2, hd.jobs - 1)];
-        const int ot = row - o.tok0;
-        if (ot >= 0 && ot < o.ntok) own = parts_of(o, kh, hk, hd);
-        ro = part_row(ot, hl);
-      }
+      ro = part_row(ot, hl);
       pre = parts_of(j, kh, hk, hd);
+      own = parts_of(o, kh, hk, hd);
     }
     join_row<D, HALF>(a, p, pre, rp, own, ro, row, hq, lane);
   }
@@ -1608,7 +1596,7 @@ size_t carve(const KvAttendArgs& a, int ctas, unsigned char* ws, KvPlan& p) {
   };
   take(p.head, 1);
   take(p.jobs, (size_t)p.cap + 1);
-  take(p.job0, n);
+  take(p.shared, G ? (size_t)a.b.n_tokens : 0);
   take(p.gjob, G > PLAN_GROUPS ? G : 0);
   take(p.gsum, G > PLAN_GROUPS ? 4 * G : 0);
   take(p.start, ctas);
