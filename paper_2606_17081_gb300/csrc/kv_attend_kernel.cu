@@ -18,7 +18,7 @@
 // What bounds it (one GB300): single tokens over long contexts, HBM (256 requests
 // of 256 to 8192 own tokens, 8 kv heads of 128: 2.4 GB in 358 us, 6.7 TB/s); prompts
 // and prefixes that many rows share, the tensor cores (4096 tokens behind 12 288,
-// 32 heads: 620 us, 1.55 PFLOP/s, 128 keys for 256 rows in 1.3 us of which the
+// 32 heads: 637 us, 1.51 PFLOP/s, 128 keys for 256 rows in 1.3 us of which the
 // products alone take 1.05); short steps, the chain plan - loads - product - softmax -
 // product - stores - join (one token over 701 keys: 14 us).
 #include <cuda.h>
@@ -41,7 +41,7 @@ constexpr int TK = 128;        // keys of a tile
 // takes 1.3 us, a narrow one 0.8 us from L2 and 1.4 us where all SMs wait for HBM.
 // 64 requests on a prefix of 32 768, 8 groups of 256 in all, 6 prompts of 100 to
 // 2047 on a prefix: 83, 427, 259 us; with 4, 6, 3, 10: 86, 427, 273 us; with equal
-// tiles and OV 2 for all: 142, 524, 299 us (on an earlier kernel).
+// tiles and OV 2 for all, on an earlier kernel: 142, 524, 299 us.
 constexpr int W_NARROW = 4, W_WIDE = 5, OV_NARROW = 3, OV_WIDE = 10;
 constexpr int NT_PLAN = 1024;
 constexpr int NT_ATT = 384;
@@ -821,8 +821,8 @@ __device__ __forceinline__ void join_row(const KvAttendArgs& a, const KvPlan& p,
 // Rows that have parts, a warp a row: of the jobs that a share's end cut, and of
 // shared groups, whose rows have a prefix job and an own one.  The parts' order
 // is the keys', so the result does not depend on when they came.
-// Bound: latency (plan, lengths, jobs and parts depend on each other): 2 us for
-// the rows of one token, 5 to 8 us for the shared rows of 16 to 256.  Joining in the
+// Bound: latency (head, list, jobs and parts depend on each other): 2 us for the
+// rows of one token, 4 to 8 us for the shared rows of 8 to 33 tokens.  Joining in the
 // attention kernel, behind a barrier of all CTAs, took as long and left fewer warps
 // to it (16 rows a group on a prefix of 32 768: 49 us in all against 44 us).
 template <int D, bool HALF>
