@@ -448,7 +448,9 @@ rs_status poa_estimate_noalloc(const rs_config* cfg, const rs_records* records, 
  * tables on the device only, and neither read nor write outside the arrays
  * described here, whatever the lengths and tables hold.  The workspace of
  * kv_attend grows at a call larger than those before it (cudaMalloc), so a
- * stream capture follows one such call outside it. */
+ * stream capture follows one such call outside it (else RS_ERR_STATE, without
+ * a launch); what a capture holds stays until route_destroy, and is shared:
+ * replays and calls of one context must not overlap on the GPU. */
 
 enum { RS_BF16 = 0, RS_FP16 = 1 };
 

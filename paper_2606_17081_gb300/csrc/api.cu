@@ -6,6 +6,7 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -50,6 +51,8 @@ struct rs_ctx {
       p_nwin, p_prob, p_wstat, p_tstat, p_wprob, p_wnext;
   DevBuf k_in, k_out;
   DevBuf kv_ws;                // kv_attend's workspace
+  bool kv_captured = false;    // a stream capture holds its address
+  std::vector<DevBuf> kv_kept; // outgrown ones that captures hold
   int32_t* kv_err = nullptr;   // pinned, written by kv_attend's kernel when a wait ran out
   DevBuf h_tokens, h_offsets, h_release, h_outlen;
   int64_t* pinned = nullptr;   // small host staging for device -> host reads
@@ -330,6 +333,7 @@ void route_destroy(rs_ctx* ctx) {
                    &ctx->i_first, &ctx->i_num, &ctx->i_ids, &ctx->i_nz, &ctx->i_count,
                    &ctx->i_stamps, &ctx->i_scratch, &ctx->kv_ws};
   for (DevBuf* b : all) release(*b);
+  for (DevBuf& b : ctx->kv_kept) release(b);
   if (ctx->pinned) cudaFreeHost(ctx->pinned);
   if (ctx->kv_err) cudaFreeHost(ctx->kv_err);
   for (auto& ev : ctx->ev)
@@ -1442,6 +1446,23 @@ rs_status kv_attend(rs_ctx* ctx, const rs_kv_cache* cache, const rs_kv_batch* ba
   for (int64_t s : {a.q_ts, a.q_hs, a.o_ts, a.o_hs})
     if (s <= 0 || s % 8 != 0 || s >= (1ll << 35))
       return fail(ctx, RS_ERR_INVALID, "q and out strides must be multiples of 8 in (0, 2^35)");
+  // A captured call's launches keep the workspace's address, so that workspace stays until the context ends.
+  cudaStreamCaptureStatus capture;
+  CK(cudaStreamIsCapturing(ctx->st, &capture), "cudaStreamIsCapturing");
+  const size_t need = kv_attend_bytes(a, ctx->sms);
+  if (capture != cudaStreamCaptureStatusNone) {
+    if (!ctx->kv_err || ctx->kv_ws.n < need)
+      return fail(ctx, RS_ERR_STATE, "a capture has to follow a kv_attend outside it that needs as much workspace");
+    ctx->kv_captured = true;
+  } else if (ctx->kv_captured && ctx->kv_ws.n < need) {
+    try {
+      ctx->kv_kept.push_back(ctx->kv_ws);
+    } catch (const std::bad_alloc&) {
+      return fail(ctx, RS_ERR_OOM, "out of host memory");
+    }
+    ctx->kv_ws = DevBuf();
+    ctx->kv_captured = false;
+  }
   if (!ctx->kv_err) {
     CK(cudaMallocHost(reinterpret_cast<void**>(&ctx->kv_err), sizeof(int32_t)), "cudaMallocHost");
     *ctx->kv_err = 0;
@@ -1450,7 +1471,7 @@ rs_status kv_attend(rs_ctx* ctx, const rs_kv_cache* cache, const rs_kv_batch* ba
     *ctx->kv_err = 0;
     return fail(ctx, RS_ERR_TIMEOUT, "an earlier kv_attend gave up waiting for its own copies or products");
   }
-  if ((r = ensure(ctx, ctx->kv_ws, kv_attend_bytes(a, ctx->sms), "attention workspace")) != RS_OK) return r;
+  if ((r = ensure(ctx, ctx->kv_ws, need, "attention workspace")) != RS_OK) return r;
   CK(launch_kv_attend(a, ctx->kv_ws.p, ctx->kv_err, ctx->sms, ctx->st), "attention launch");
   return RS_OK;
 }

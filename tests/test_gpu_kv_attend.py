@@ -309,6 +309,48 @@ def test_on_another_stream_and_in_a_graph():
     c.close()
 
 
+def test_a_capture_keeps_its_workspace():
+    """A capture that would have to allocate is refused; a captured step replays after larger calls."""
+    st = torch.cuda.Stream()
+    c = rs.Context(W=1, K=1024, stream=st.cuda_stream)
+    small, large = Step(21, [1, 2], [40, 300], 8, 2, 64, BF), Step(22, [400, 3], [900, 2000], 16, 4, 128, BF)
+    (cache, batch, q), big = small.to(rs), large.to(rs)
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    out2, lse2 = torch.empty_like(big[2]), torch.empty(big[2].shape[:2], device="cuda")
+    torch.cuda.synchronize()
+
+    def refused(cache, batch, q, out, lse):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=st):
+            with pytest.raises(rs.RoutesimError) as e:
+                rs.kv_attend(c.h, cache, batch, q, small.scale, out, lse)
+        assert e.value.status == rs.RS_ERR_STATE
+
+    refused(cache, batch, q, out, lse)
+    with torch.cuda.stream(st):
+        rs.kv_attend(c.h, cache, batch, q, small.scale, out, lse)
+    st.synchronize()
+    refused(*big, out2, lse2)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=st):
+        rs.kv_attend(c.h, cache, batch, q, small.scale, out, lse)
+    with torch.cuda.stream(st):
+        rs.kv_attend(c.h, *big, large.scale, out2, lse2)
+    fill = [torch.full((1 << 22,), float("nan"), device="cuda") for _ in range(8)]   # (what a freed workspace could become)
+    for _ in range(2):
+        out.fill_(7)
+        lse.fill_(7)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(st):
+            g.replay()
+            rs.kv_attend(c.h, *big, large.scale, out2, lse2)
+        st.synchronize()
+        compare(small, out, lse)
+        compare(large, out2, lse2)
+    assert all(bool(x.isnan().all()) for x in fill)
+    c.close()
+
+
 def test_refusals(ctx):
     s = Step(15, [1], [9], 4, 2, 64, BF)
     cache, batch, q = s.to(rs)
