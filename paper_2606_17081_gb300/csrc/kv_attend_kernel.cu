@@ -727,19 +727,26 @@ struct Parts {
   int c0, first, last, count;
 };
 
-__device__ __forceinline__ Parts parts_of(const KvJob& j, int head, int n_kv_heads, const KvHead& hd) {
-  Parts r{0, 0, 0, 0};
-  if (j.nt <= 0) return r;
+// By a warp: of job j in lanes 0..15 and of job j in lanes 16..31, with a share of the
+// arithmetic a lane (a job's first CTA in lanes 0 and 16, its last one in 8 and 24).
+__device__ __forceinline__ void parts_of(const KvJob& j, int head, int n_kv_heads, const KvHead& hd, int lane, Parts& x, Parts& y) {
+  const bool end = lane & 8;
   const int cost = job_cost(j.nt, j.flags);
   const int64_t u0 = j.cost * n_kv_heads + (int64_t)head * cost;
-  const int64_t c0 = quotient(u0, hd.per), c1 = quotient(u0 + cost - 1, hd.per);
+  const int64_t c = quotient(end ? u0 + cost - 1 : u0, hd.per);
   int t0, t1;
-  r.c0 = (int)c0;
-  r.first = (int)(segment(u0, cost, j.flags, j.nt, hd.per, c0, t0, t1) ? c0 : c0 + 1);
-  r.last = (int)(segment(u0, cost, j.flags, j.nt, hd.per, c1, t0, t1) ? c1 : c1 - 1);
-  r.count = max(r.last - r.first + 1, 1);
-  if (r.count == 1) r.last = r.first - 1;
-  return r;
+  const int in = (int)(segment(u0, cost, j.flags, j.nt, hd.per, c, t0, t1) ? c : end ? c - 1 : c + 1);
+  auto gather = [&](int from) {
+    Parts r;
+    r.c0 = (int)__shfl_sync(~0u, (int)c, from);
+    r.first = __shfl_sync(~0u, in, from);
+    r.last = __shfl_sync(~0u, in, from + 8);
+    r.count = max(r.last - r.first + 1, 1);
+    if (r.count == 1) r.last = r.first - 1;
+    return __shfl_sync(~0u, j.nt, from) > 0 ? r : Parts{0, 0, 0, 0};
+  };
+  x = gather(0);
+  y = gather(16);
 }
 
 // One row (token, head) from its parts: x's (row rx of the 256 if cut, else at
@@ -848,19 +855,18 @@ __global__ void __launch_bounds__(256) k_kv_join(const __grid_constant__ KvAtten
       hq = c.head * p.ratio + hl;
       rp = part_row(tok, hl);
     } else {
-      const int64_t t = (x - cuts) / a.n_heads;
+      const int64_t t = quotient(x - cuts, a.n_heads);
       hq = (int)(x - cuts - t * a.n_heads);
       const int4 e = p.shared[t];
       // (starts that decrease leave entries unwritten)
       if (e.y < 0 || e.y >= hd.prefix_jobs || e.z < 0 || e.z >= hd.jobs) continue;
-      const KvJob j = p.jobs[e.y], o = p.jobs[e.z];
-      const int kh = hq / p.ratio, hl = hq - kh * p.ratio, tok = e.x - j.tok0, ot = e.x - o.tok0;
-      if (tok < 0 || tok >= j.ntok || ot < 0 || ot >= o.ntok) continue;
+      const KvJob j = p.jobs[lane < 16 ? e.y : e.z];
+      const int kh = hq / p.ratio, hl = hq - kh * p.ratio, tok = e.x - j.tok0, at = part_row(tok, hl);
+      if (__any_sync(~0u, tok < 0 || tok >= j.ntok)) continue;
       row = e.x;
-      rp = part_row(tok, hl);
-      ro = part_row(ot, hl);
-      pre = parts_of(j, kh, hk, hd);
-      own = parts_of(o, kh, hk, hd);
+      rp = __shfl_sync(~0u, at, 0);
+      ro = __shfl_sync(~0u, at, 16);
+      parts_of(j, kh, hk, hd, lane, pre, own);
     }
     join_row<D, HALF>(a, p, pre, rp, own, ro, row, hq, lane);
   }
