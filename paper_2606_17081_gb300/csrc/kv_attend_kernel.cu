@@ -751,8 +751,8 @@ __device__ __forceinline__ void parts_of(const KvJob& j, int head, int n_kv_head
 
 // One row (token, head) from its parts: x's (row rx of the 256 if cut, else at
 // home), then y's.  A lane takes the log sum of a part, the warp their largest
-// and the weights, and the rows of several parts are on their way at once.
-template <int D, bool HALF>
+// and the weights, and the rows of Z parts are on their way at once.
+template <int D, bool HALF, int Z>
 __device__ __forceinline__ void join_row(const KvAttendArgs& a, const KvPlan& p, const Parts& x, int rx, const Parts& y, int ry,
                                          int64_t row, int hq, int lane) {
   constexpr int E = D / 32;
@@ -775,10 +775,10 @@ __device__ __forceinline__ void join_row(const KvAttendArgs& a, const KvPlan& p,
       src = (whole ? p.home : p.part) + at * D;
     }
     float wt = 0.0f;
-    for (int q = 0; q < here; q += 8) {
-      float v[8][E];
+    for (int q = 0; q < here; q += Z) {
+      float v[Z][E];
 #pragma unroll
-      for (int z = 0; z < 8; z++) {   // (past the last part: weight 0, the last one's row)
+      for (int z = 0; z < Z; z++) {   // (past the last part: weight 0, the last one's row)
         const int from = min(q + z, here - 1);
         const float* r = reinterpret_cast<const float*>(__shfl_sync(~0u, reinterpret_cast<unsigned long long>(src), from)) + lane * E;
         if constexpr (E == 4) {
@@ -805,7 +805,7 @@ __device__ __forceinline__ void join_row(const KvAttendArgs& a, const KvPlan& p,
         m = m2;
       }
 #pragma unroll
-      for (int z = 0; z < 8; z++) {
+      for (int z = 0; z < Z; z++) {
         const float w = __shfl_sync(~0u, wt, min(q + z, here - 1));
         if (q + z < here && w != 0.0f) {
 #pragma unroll
@@ -832,7 +832,7 @@ __device__ __forceinline__ void join_row(const KvAttendArgs& a, const KvPlan& p,
 // rows of one token, 4 to 8 us for the shared rows of 8 to 33 tokens.  Joining in the
 // attention kernel, behind a barrier of all CTAs, took as long and left fewer warps
 // to it (16 rows a group on a prefix of 32 768: 49 us in all against 44 us).
-template <int D, bool HALF>
+template <int D, bool HALF, int Z>
 __global__ void __launch_bounds__(256) k_kv_join(const __grid_constant__ KvAttendArgs a,
                                                  const __grid_constant__ KvPlan p) {
   behind_stream();
@@ -847,7 +847,7 @@ __global__ void __launch_bounds__(256) k_kv_join(const __grid_constant__ KvAtten
     Parts pre{0, 0, 0, 0}, own{0, 0, 0, 0};
     int row, hq, rp, ro = 0;
     if (x < cuts) {
-      const int u = (int)(x / hd.cut_rows), r = (int)(x - (int64_t)u * hd.cut_rows), tok = r / p.ratio, hl = r - tok * p.ratio;
+      const int u = (int)quotient(x, hd.cut_rows), r = (int)(x - (int64_t)u * hd.cut_rows), tok = r / p.ratio, hl = r - tok * p.ratio;
       const KvCut c = p.cut[u];
       if (tok >= c.ntok) continue;
       pre = Parts{c.c0, c.first, c.last, c.last - c.first + 1};
@@ -868,7 +868,7 @@ __global__ void __launch_bounds__(256) k_kv_join(const __grid_constant__ KvAtten
       ro = __shfl_sync(~0u, at, 16);
       parts_of(j, kh, hk, hd, lane, pre, own);
     }
-    join_row<D, HALF>(a, p, pre, rp, own, ro, row, hq, lane);
+    join_row<D, HALF, Z>(a, p, pre, rp, own, ro, row, hq, lane);
   }
 }
 
@@ -1632,7 +1632,11 @@ cudaError_t run(const KvAttendArgs& a, const KvPlan& p, const CUtensorMap* m, cu
   // a warp a row, no more than the GPU holds at once
   const int64_t rows = std::min<int64_t>((int64_t)p.ctas * 256, (int64_t)a.b.n_tokens * a.n_heads) +
                        (a.b.n_groups ? (int64_t)a.b.n_tokens * a.n_heads : 0);
-  return launch_behind(k_kv_join<D, HALF>, (unsigned)std::min<int64_t>((rows + 7) / 8, (int64_t)p.ctas * 8), 256, 0, st, a, p);
+  // Few rows: eight parts of each on their way at once (111 registers, 16 rows an SM); many: four (75 registers, 24 rows).
+  // Eight and four, us a call in a replayed graph: 256 tokens x heads behind a prefix 17.9 and 18.2, 924 23.6 and 24.1,
+  // 4096 85.1 and 84.4, 8192 411 and 408, 6 prompts' 200 000 263 and 256
+  auto join = rows < (int64_t)p.ctas * 48 ? k_kv_join<D, HALF, 8> : k_kv_join<D, HALF, 4>;
+  return launch_behind(join, (unsigned)std::min<int64_t>((rows + 7) / 8, (int64_t)p.ctas * 8), 256, 0, st, a, p);
 }
 
 }  // namespace

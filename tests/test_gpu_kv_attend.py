@@ -309,6 +309,14 @@ def test_on_another_stream_and_in_a_graph():
     c.close()
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_many_rows_of_many_parts(ctx, dim, dtype):
+    """9600 rows to join, a prefix's jobs over seven CTAs or so each, own parts of one tile."""
+    s = Step(23, [149, 0, 151], [4100, 4096, 4111], 16, 4, dim, dtype, group_start=[0, 3], prefix=[4096])
+    compare(s, *attend(ctx, s))
+
+
 def test_a_capture_keeps_its_workspace():
     """A capture that would have to allocate is refused; a captured step replays after larger calls."""
     st = torch.cuda.Stream()
