@@ -18,7 +18,7 @@
 // What bounds it (one GB300): single tokens over long contexts, HBM (256 requests
 // of 256 to 8192 own tokens, 8 kv heads of 128: 2.4 GB in 358 us, 6.7 TB/s); prompts
 // and prefixes that many rows share, the tensor cores (4096 tokens behind 12 288,
-// 32 heads: 637 us, 1.51 PFLOP/s, 128 keys for 256 rows in 1.3 us of which the
+// 32 heads: 634 us, 1.52 PFLOP/s, 128 keys for 256 rows in 1.3 us of which the
 // products alone take 1.05); short steps, the chain plan - loads - product - softmax -
 // product - stores - join (one token over 701 keys: 14 us).
 #include <cuda.h>
@@ -828,8 +828,9 @@ __device__ __forceinline__ void join_row(const KvAttendArgs& a, const KvPlan& p,
 // Rows that have parts, a warp a row: of the jobs that a share's end cut, and of
 // shared groups, whose rows have a prefix job and an own one.  The parts' order
 // is the keys', so the result does not depend on when they came.
-// Bound: latency (head, list, jobs and parts depend on each other): 2 us for the
-// rows of one token, 4 to 8 us for the shared rows of 8 to 33 tokens.  Joining in the
+// Bound: latency (head, list, jobs and parts depend on each other) and, past a few
+// rows a warp, arithmetic: 2 us for the rows of one token, 3 to 6 us for the shared rows
+// of 8 to 64 tokens (1 to 2 us more when every lane found all parts' places itself).  Joining in the
 // attention kernel, behind a barrier of all CTAs, took as long and left fewer warps
 // to it (16 rows a group on a prefix of 32 768: 49 us in all against 44 us).
 template <int D, bool HALF, int Z>
