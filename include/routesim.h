@@ -540,6 +540,8 @@ rs_status kv_append(rs_ctx* ctx, const rs_kv_cache* cache, const void* k_dev, co
  * cache reads as a block of zeros.  What lies in the blocks past kv_len does
  * not matter, NaN included; K and V of the kv_len tokens have to be finite
  * (0 times an infinity in a masked position of the same request is NaN).
+ * A q that is not finite leaves its own row of out and lse unspecified (NaN as
+ * a rule) and no other.
  * RS_ERR_TIMEOUT: a kernel of an earlier call gave up on a bounded wait (its
  * outputs are unspecified); reported once, without doing this call's work. */
 rs_status kv_attend(rs_ctx* ctx, const rs_kv_cache* cache, const rs_kv_batch* batch,
