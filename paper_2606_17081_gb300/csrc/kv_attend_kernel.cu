@@ -99,9 +99,9 @@ struct KvPlan {
   KvStart* start;       // [ctas]
   KvCut* cut;           // [ctas] the cut jobs, in any order
   float* part;          // [ctas][2][256][D] cut jobs' rows: of the first cut job (0), of the last (1)
-  float* part_lse;      // [ctas][2][256]
+  float2* part_sum;     // [ctas][2][256] of each its reference (a power of two's exponent) and its weights' sum
   float* home;          // [2][rows][D] rows with a prefix job and an own one, each whole
-  float* home_lse;      // [2][rows]
+  float2* home_sum;     // [2][rows]
   int32_t* err;         // host memory: set when a wait ran out
   int32_t cap;          // jobs at most
   int32_t ctas;
@@ -798,8 +798,10 @@ __device__ __forceinline__ void parts_of(const KvJob& j, int head, int n_kv_head
 }
 
 // One row (token, head) from its parts: x's (row rx of the 256 if cut, else at
-// home), then y's.  A lane takes the log sum of a part, the warp their largest
-// and the weights, and the rows of Z parts are on their way at once.
+// home), then y's.  A lane takes the reference and sum of a part, the warp the
+// largest reference and the weights, and the rows of Z parts are on their way at
+// once.  (Log sums in their place would lose the sums where scores are large: at
+// 2^24 a log sum has steps of 2.)
 template <int D, bool HALF, int Z>
 __device__ __forceinline__ void join_row(const KvAttendArgs& a, const KvPlan& p, const Parts& x, int rx, const Parts& y, int ry,
                                          int64_t row, int hq, int lane) {
@@ -812,14 +814,14 @@ __device__ __forceinline__ void join_row(const KvAttendArgs& a, const KvPlan& p,
   for (int base = 0; base < count; base += 32) {
     const int k = base + lane, here = min(32, count - base);
     const float* src = nullptr;
-    float s = -INFINITY;
+    float2 s = make_float2(-INFINITY, 0.0f);
     if (k < count) {
       const Parts& q = k < x.count ? x : y;
       const int c = q.first + (k < x.count ? k : k - x.count);
       const bool whole = q.last < q.first;
       const int64_t at = whole ? (k < x.count ? 0 : all) + home
                                : ((int64_t)c * 2 + (c == q.c0 ? 1 : 0)) * 256 + (k < x.count ? rx : ry);
-      s = (whole ? p.home_lse : p.part_lse)[at];
+      s = (whole ? p.home_sum : p.part_sum)[at];
       src = (whole ? p.home : p.part) + at * D;
     }
     float wt = 0.0f;
@@ -838,12 +840,12 @@ __device__ __forceinline__ void join_row(const KvAttendArgs& a, const KvPlan& p,
         }
       }
       if (q == 0) {   // the weights, with the first rows on their way
-        float big = s;
+        float big = s.x;
 #pragma unroll
         for (int z = 16; z; z >>= 1) big = fmaxf(big, __shfl_xor_sync(~0u, big, z));
         const float m2 = fmaxf(m, big);
         const float f = m == -INFINITY ? 0.0f : ex2(__fsub_rn(m, m2));
-        wt = s == -INFINITY ? 0.0f : ex2(__fsub_rn(s, m2));
+        wt = s.y == 0.0f ? 0.0f : __fmul_rn(s.y, ex2(__fsub_rn(s.x, m2)));
         float sum = wt;
 #pragma unroll
         for (int z = 16; z; z >>= 1) sum = __fadd_rn(sum, __shfl_xor_sync(~0u, sum, z));
@@ -1476,7 +1478,7 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
                                  : ((int64_t)blockIdx.x * 2 + (g.cut_front ? 0 : 1)) * 256 + (wide ? s * 128 : 0) + r;
         float* part = (whole ? p.home : p.part) + at * D;
         if (live) {
-          if (!direct) (whole ? p.home_lse : p.part_lse)[at] = lse2;
+          if (!direct) (whole ? p.home_sum : p.part_sum)[at] = make_float2(l == 0.0f ? -INFINITY : __fmul_rn(m, sl), l);
           else if (a.lse) a.lse[(int64_t)row * a.n_heads + hq] = __fmul_rn(lse2, 0.6931471805599453f);
         }
         const unsigned lives = __ballot_sync(~0u, live);
@@ -1641,9 +1643,9 @@ size_t carve(const KvAttendArgs& a, int ctas, unsigned char* ws, KvPlan& p) {
   take(p.start, ctas);
   take(p.cut, ctas);
   take(p.part, (size_t)ctas * 2 * 256 * D);
-  take(p.part_lse, (size_t)ctas * 2 * 256);
+  take(p.part_sum, (size_t)ctas * 2 * 256);
   take(p.home, G ? 2 * rows * D : 0);
-  take(p.home_lse, G ? 2 * rows : 0);
+  take(p.home_sum, G ? 2 * rows : 0);
   return o;
 }
 

@@ -27,7 +27,8 @@ def past_its_maximum(scale, least, most):
 
 
 @pytest.mark.parametrize("dim", [64, 128])
-@pytest.mark.parametrize("new,ctxs,groups", [([1], [700], None), ([70], [300], None), ([3, 1, 200], [0, 40, 500], None)])
+@pytest.mark.parametrize("new,ctxs,groups", [([1], [700], None), ([70], [300], None), ([1] * 6, [260, 300, 256, 290, 400, 257], ([0, 6], [256])),
+                                             ([3, 1, 200], [0, 40, 500], None)])
 def test_rows_of_nan_beside_rows_of_huge_scores(ctx, dim, new, ctxs, groups):  # noqa: F811
     """Of each kv head's four heads one is NaN, one has finite scores of some 2^35, two are ordinary."""
     s = Step(31, new, ctxs, 8, 2, dim, BF, *(groups or ()))
