@@ -668,6 +668,25 @@ __device__ __forceinline__ float max3(float a, uint32_t b, uint32_t c) {
   return r;
 }
 
+// The largest score of a row's tile, of which the warp's rows see `seen` keys at
+// most and this one `left`.
+__device__ __noinline__ float row_max(uint32_t ts, int seen, int left) {
+  float m = -INFINITY, n = -INFINITY;
+#pragma unroll 1
+  for (int c = 0; c < min(seen, TK); c += 32) {
+    uint32_t x[32];
+    tm_ld32(x, ts + c);
+    tm_wait_ld(x);
+    cut32(x, left - c);
+#pragma unroll
+    for (int k = 0; k < 32; k += 4) {
+      m = max3(m, x[k], x[k + 1]);
+      n = max3(n, x[k + 2], x[k + 3]);
+    }
+  }
+  return fmaxf(m, n);
+}
+
 __device__ __forceinline__ float max_of32(const uint32_t* v) {
   float m = __uint_as_float(v[0]), n = __uint_as_float(v[31]);
 #pragma unroll
@@ -699,73 +718,6 @@ __device__ __forceinline__ void row_exp(float sl, float nm, uint32_t* v, float& 
 }
 
 __device__ __forceinline__ float minus(float m, float sl) { return m == -INFINITY ? 0.0f : -__fmul_rn(m, sl); }
-
-struct RowSums {
-  float m, l0, l1;   // the row's reference and sums so far
-  float a0, a1;      // the tile's sums
-};
-
-// A tile for the second and last time, where the weights of some rows of the warp (move) sum to too much or
-// have no reference yet: those rows' m moves to the tile's maximum, O (unless it holds nothing yet) and l are
-// scaled, and all weights are written.  No reference would do better than the maximum, so nothing is looked at again:
-// infinities and NaN in a row end here as in any other.  A row that does not move keeps its sums, and its weights
-// come out as they were, so it does not depend on the rows beside it.
-template <int D, bool HALF>
-__device__ __noinline__ RowSums row_again(uint32_t ts, uint32_t to, int seen, int left, float sl, bool first, bool move, RowSums r) {
-  float x = -INFINITY, y = -INFINITY;
-#pragma unroll 1
-  for (int c = 0; c < min(seen, TK); c += 32) {
-    uint32_t v[32];
-    tm_ld32(v, ts + c);
-    tm_wait_ld(v);
-    cut32(v, left - c);
-#pragma unroll
-    for (int k = 0; k < 32; k += 4) {
-      x = max3(x, v[k], v[k + 1]);
-      y = max3(y, v[k + 2], v[k + 3]);
-    }
-  }
-  const float m = move ? fmaxf(r.m, fmaxf(x, y)) : r.m;
-  const bool moved = m > r.m;
-  if (!first && __any_sync(~0u, moved)) {
-    const float f = moved ? ex2(__fmul_rn(__fsub_rn(r.m, m), sl)) : 1.0f;
-    r.l0 = __fmul_rn(r.l0, f);
-    r.l1 = __fmul_rn(r.l1, f);
-#pragma unroll 1
-    for (int c = 0; c < D; c += 32) {
-      uint32_t o[32];
-      tm_ld32(o, to + c);
-      tm_wait_ld(o);
-#pragma unroll
-      for (int k = 0; k < 32; k++) o[k] = __float_as_uint(__fmul_rn(__uint_as_float(o[k]), f));
-      tm_st32(to + c, o);
-    }
-  }
-  const float nm = minus(m, sl);
-  float a0 = 0.0f, a1 = 0.0f;
-#pragma unroll 1
-  for (int c = 0; c < TK; c += 64) {   // (the weights' columns have been read before they are written)
-    uint32_t w[32];
-#pragma unroll
-    for (int h = 0; h < 64; h += 32) {
-      uint32_t v[32];
-#pragma unroll
-      for (int k = 0; k < 32; k++) v[k] = 0;
-      if (c + h < seen) {
-        tm_ld32(v, ts + c + h);
-        tm_wait_ld(v);
-        cut32(v, left - c - h);
-        row_exp<HALF, 8>(sl, nm, v, a0, a1);
-      }
-#pragma unroll
-      for (int k = 0; k < 16; k++) w[h / 2 + k] = v[k];
-    }
-    tm_st32(ts + c / 2, w);
-  }
-  r.m = m;
-  if (moved) { r.a0 = a0; r.a1 = a1; }
-  return r;
-}
 
 // ------------------------------------------------------------------ joining
 
@@ -1371,58 +1323,76 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
         if (any) {
           const int k0 = (g.t0 + t) * TK, left = lim - k0, seen = high - k0;
           const bool first = i == 0;   // O holds nothing yet
-          bool again;
-          RowSums x = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-          // (m from a row's first keys will do)
-          if (low >= k0 + TK) {
-            uint32_t v[128];
+          float a0, a1;
+          // Twice at most: where some row's weights sum to too much, or it has no m yet, its m moves to the tile's maximum
+          // and all weights are taken again (the other rows' come out as they were).  No m would do better than the
+          // maximum, so the second pass is not looked at: infinities and NaN in a row end here as in any other.
+#pragma unroll 1
+          for (int pass = 0; pass < 2; pass++) {
+            a0 = a1 = 0.0f;
+            // (m from a row's first keys will do)
+            if (low >= k0 + TK) {
+              uint32_t v[128];
 #pragma unroll
-            for (int c = 0; c < TK; c += 32) tm_ld32(v + c, ts + c);
+              for (int c = 0; c < TK; c += 32) tm_ld32(v + c, ts + c);
 #pragma unroll
-            for (int c = 0; c < TK; c += 32) tm_wait_ld(v + c);
-            if (first && m == -INFINITY) m = max_of32(v);
-            row_exp<HALF, 32>(sl, minus(m, sl), v, x.a0, x.a1);
-            again = __any_sync(~0u, (live && __fadd_rn(x.a0, x.a1) > 32768.0f) || m == -INFINITY);
-            if (!again) {
-              tm_st32(ts, v);
-              tm_st32(ts + 32, v + 32);
-            }
-          } else {
-            // the warp's rows see different ends: 32 keys at a time, up to the last that one sees
-            uint32_t w[64];
+              for (int c = 0; c < TK; c += 32) tm_wait_ld(v + c);
+              if (first && m == -INFINITY) m = max_of32(v);
+              row_exp<HALF, 32>(sl, minus(m, sl), v, a0, a1);
+              const bool over = live && __fadd_rn(a0, a1) > 32768.0f;
+              if (pass || !__any_sync(~0u, over || m == -INFINITY)) {
+                tm_st32(ts, v);
+                tm_st32(ts + 32, v + 32);
+                break;
+              }
+            } else {
+              // the warp's rows see different ends: 32 keys at a time, up to the last that one sees
+              uint32_t w[64];
 #pragma unroll
-            for (int c = 0; c < 64; c++) w[c] = 0;
+              for (int c = 0; c < 64; c++) w[c] = 0;
 #pragma unroll
-            for (int c = 0; c < TK; c += 32) {
-              if (c < seen) {
-                uint32_t v[32];
-                tm_ld32(v, ts + c);
-                tm_wait_ld(v);
-                cut32(v, left - c);
-                if (c == 0 && first && m == -INFINITY) m = max_of32(v);
-                row_exp<HALF, 8>(sl, minus(m, sl), v, x.a0, x.a1);
+              for (int c = 0; c < TK; c += 32) {
+                if (c < seen) {
+                  uint32_t v[32];
+                  tm_ld32(v, ts + c);
+                  tm_wait_ld(v);
+                  cut32(v, left - c);
+                  if (c == 0 && first && m == -INFINITY) m = max_of32(v);
+                  row_exp<HALF, 8>(sl, minus(m, sl), v, a0, a1);
 #pragma unroll
-                for (int k = 0; k < 16; k++) w[c / 2 + k] = v[k];
+                  for (int k = 0; k < 16; k++) w[c / 2 + k] = v[k];
+                }
+              }
+              const bool over = live && __fadd_rn(a0, a1) > 32768.0f;
+              if (pass || !__any_sync(~0u, over || (m == -INFINITY && left > 0))) {
+                tm_st32(ts, w);
+                tm_st32(ts + 32, w + 32);
+                break;
               }
             }
-            again = __any_sync(~0u, (live && __fadd_rn(x.a0, x.a1) > 32768.0f) || (m == -INFINITY && left > 0));
-            if (!again) {
-              tm_st32(ts, w);
-              tm_st32(ts + 32, w + 32);
+            // a row's m moves: O and l are scaled
+            const bool over = live && __fadd_rn(a0, a1) > 32768.0f, none = m == -INFINITY && left > 0;
+            const float x = row_max(ts, seen, left);
+            const float m2 = over || none ? fmaxf(m, x) : m;
+            const bool moved = __any_sync(~0u, m2 > m);
+            const float f = m2 > m ? ex2(__fmul_rn(__fsub_rn(m, m2), sl)) : 1.0f;
+            if (!first && moved) {
+              l0 = __fmul_rn(l0, f);
+              l1 = __fmul_rn(l1, f);
+#pragma unroll 1
+              for (int c = 0; c < D; c += 32) {
+                uint32_t o[32];
+                tm_ld32(o, tmem + lanes + 256 + s * D + c);
+                tm_wait_ld(o);
+#pragma unroll
+                for (int k = 0; k < 32; k++) o[k] = __float_as_uint(__fmul_rn(__uint_as_float(o[k]), f));
+                tm_st32(tmem + lanes + 256 + s * D + c, o);
+              }
             }
+            m = m2;
           }
-          if (again) {
-            const bool move = live && (__fadd_rn(x.a0, x.a1) > 32768.0f || (m == -INFINITY && left > 0));
-            x.m = m;
-            x.l0 = l0;
-            x.l1 = l1;
-            x = row_again<D, HALF>(ts, tmem + lanes + 256 + s * D, seen, left, sl, first, move, x);
-            m = x.m;
-            l0 = x.l0;
-            l1 = x.l1;
-          }
-          l0 = __fadd_rn(l0, x.a0);
-          l1 = __fadd_rn(l1, x.a1);
+          l0 = __fadd_rn(l0, a0);
+          l1 = __fadd_rn(l1, a1);
           tm_wait_st();
         }
         if (ends && t == g.nt() - 1 && !(wide && s)) {
