@@ -719,6 +719,42 @@ __device__ __forceinline__ void row_exp(float sl, float nm, uint32_t* v, float& 
 
 __device__ __forceinline__ float minus(float m, float sl) { return m == -INFINITY ? 0.0f : -__fmul_rn(m, sl); }
 
+// References so large that m sl rounds by more than a half: a weight exp2(sl s + nm) then carries that rounding, which
+// may be more than a type's range.
+constexpr float FAR = 16777216.0f;
+
+// A tile's weights where some row of the warp is that far (m of each row at its tile's maximum): exp2(sl (s - m)),
+// which the largest score makes 1 whatever its size.  The other rows' weights are the same as elsewhere.
+template <bool HALF>
+__device__ __noinline__ float2 far_weights(uint32_t ts, int seen, int left, float sl, float m) {
+  const float nm = minus(m, sl);
+  const bool far = fabsf(nm) > FAR;
+  float a0 = 0.0f, a1 = 0.0f;
+#pragma unroll 1
+  for (int c = 0; c < TK; c += 64) {   // (the weights' columns have been read before they are written)
+    uint32_t w[32];
+#pragma unroll
+    for (int h = 0; h < 64; h += 32) {
+      uint32_t v[32];
+#pragma unroll
+      for (int k = 0; k < 32; k++) v[k] = 0;
+      if (c + h < seen) {
+        tm_ld32(v, ts + c + h);
+        tm_wait_ld(v);
+        cut32(v, left - c - h);
+#pragma unroll
+        for (int k = 0; k < 32; k++)
+          if (far) v[k] = __float_as_uint(__fsub_rn(__uint_as_float(v[k]), m));
+        row_exp<HALF, 8>(sl, far ? 0.0f : nm, v, a0, a1);
+      }
+#pragma unroll
+      for (int k = 0; k < 16; k++) w[h / 2 + k] = v[k];
+    }
+    tm_st32(ts + c / 2, w);
+  }
+  return make_float2(a0, a1);
+}
+
 // ------------------------------------------------------------------ joining
 
 // Where the parts of a job and head are: whole in its place among all rows (one
@@ -1338,8 +1374,9 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
 #pragma unroll
               for (int c = 0; c < TK; c += 32) tm_wait_ld(v + c);
               if (first && m == -INFINITY) m = max_of32(v);
-              row_exp<HALF, 32>(sl, minus(m, sl), v, a0, a1);
-              const bool over = live && __fadd_rn(a0, a1) > 32768.0f;
+              const float nm = minus(m, sl);
+              row_exp<HALF, 32>(sl, nm, v, a0, a1);
+              const bool over = live && (__fadd_rn(a0, a1) > 32768.0f || fabsf(nm) > FAR);
               if (pass || !__any_sync(~0u, over || m == -INFINITY)) {
                 tm_st32(ts, v);
                 tm_st32(ts + 32, v + 32);
@@ -1363,7 +1400,7 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
                   for (int k = 0; k < 16; k++) w[c / 2 + k] = v[k];
                 }
               }
-              const bool over = live && __fadd_rn(a0, a1) > 32768.0f;
+              const bool over = live && (__fadd_rn(a0, a1) > 32768.0f || fabsf(minus(m, sl)) > FAR);
               if (pass || !__any_sync(~0u, over || (m == -INFINITY && left > 0))) {
                 tm_st32(ts, w);
                 tm_st32(ts + 32, w + 32);
@@ -1371,7 +1408,7 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
               }
             }
             // a row's m moves: O and l are scaled
-            const bool over = live && __fadd_rn(a0, a1) > 32768.0f, none = m == -INFINITY && left > 0;
+            const bool over = live && (__fadd_rn(a0, a1) > 32768.0f || fabsf(minus(m, sl)) > FAR), none = m == -INFINITY && left > 0;
             const float x = row_max(ts, seen, left);
             const float m2 = over || none ? fmaxf(m, x) : m;
             const bool moved = __any_sync(~0u, m2 > m);
@@ -1390,6 +1427,12 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
               }
             }
             m = m2;
+            if (__any_sync(~0u, live && fabsf(minus(m, sl)) > FAR)) {
+              const float2 y = far_weights<HALF>(ts, seen, left, sl, m);
+              a0 = y.x;
+              a1 = y.y;
+              break;
+            }
           }
           l0 = __fadd_rn(l0, a0);
           l1 = __fadd_rn(l1, a1);
