@@ -504,7 +504,8 @@ typedef struct {
  *   slots_dev: int64 [n_tokens], 16 * block + position % 16; -1 on rows of no
  *     request, without a block, or past the table's row;
  *   counts_dev: int64 [2]: blocks the step needs (with more than n_free the
- *     rest is missing above), and its tokens (rows past n_tokens are left out).
+ *     rest is missing above), and its tokens (rows past n_tokens are left out;
+ *     q_start counts them, up to 2^31 - 1).
  * Outputs must not overlap inputs. */
 rs_status kv_tables(rs_ctx* ctx, const rs_kv_batch* batch, const int32_t* q_len_dev,
                     const int32_t* prev_len_dev, const int32_t* prefix_blocks_dev,
@@ -525,8 +526,9 @@ rs_status kv_append(rs_ctx* ctx, const rs_kv_cache* cache, const void* k_dev, co
  *   out[r][h] = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale q[r][h] . k_j),
  *   lse[r][h] = log sum_j p_j,
  * over positions j <= kv_len[i] - q_len + t with q_len = q_start[i+1] -
- * q_start[i] (the new tokens' K and V are in the cache: kv_append first).  A
- * row without any position, or of no request, gets 0 and -inf.  Scores,
+ * q_start[i] (the new tokens' K and V are in the cache: kv_append first; where
+ * the rows end inside a request, q_start past n_tokens, the tokens left out are
+ * not looked at).  A row without any position, or of no request, gets 0 and -inf.  Scores,
  * softmax statistics and sums are in 32 bits; the weights p_j are rounded to
  * the cache's type for the product with V, and out once at the end.
  *   q_dev: [n_tokens][n_heads][head_dim] of the cache's type, strides in

@@ -157,7 +157,7 @@ __device__ JobSum<Int> block_scan(JobSum<Int> x, JobSum<Int>* sm, int width, Job
 }
 
 struct ReqLens {
-  int q0, q, kv;   // first row, rows, context with them
+  int q0, q, kv;   // first row, rows, context up to the last of them (below 0: none of them sees anything)
   int g;           // group, or -1
 };
 
@@ -232,9 +232,10 @@ __device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p,
   auto rows_at = [&](int i) { return clampi(b.q_start[i], 0, b.n_tokens); };
   auto lens = [&](int i) {
     ReqLens r;
+    const int end = b.q_start[i + 1];   // (past the step's rows where they end inside the request: those tokens are not there)
     r.q0 = rows_at(i);
-    r.q = max(rows_at(i + 1) - r.q0, 0);
-    r.kv = clampi(b.kv_len[i], 0, INT_MAX - 1);
+    r.q = max(clampi(end, 0, b.n_tokens) - r.q0, 0);
+    r.kv = clampi((int64_t)max(b.kv_len[i], 0) - end + r.q0 + r.q, -(1 << 24), INT_MAX - 1);
     return r;
   };
   auto group = [&](int i) {
@@ -291,7 +292,7 @@ __device__ __forceinline__ void make_plan(const rs_kv_batch& b, const KvPlan& p,
       const unsigned top = 1u << 26, peers = __match_any_sync(__activemask(), g);
       const unsigned apart = __reduce_add_sync(peers, (unsigned)min((int64_t)rt * job_cost(tiles(seen), fl), (int64_t)top));
       const unsigned with = __reduce_add_sync(peers, (unsigned)min((int64_t)rt * job_cost(tiles(seen - P), fl), (int64_t)top));
-      const unsigned less = __reduce_or_sync(peers, r.kv - r.q + 1 < P), most = __reduce_max_sync(peers, (unsigned)r.kv);
+      const unsigned less = __reduce_or_sync(peers, r.kv - r.q + 1 < P), most = __reduce_max_sync(peers, (unsigned)max(r.kv, 0));
       if (lane == __ffs(peers) - 1) {
         atomicAdd(&sum[4 * g], (Acc)apart);
         atomicAdd(&sum[4 * g + 1], (Acc)with);
