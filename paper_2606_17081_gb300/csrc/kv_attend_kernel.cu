@@ -537,15 +537,24 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
 __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
+#ifndef KV_WAIT_CLOCKS
+#define KV_WAIT_CLOCKS (1ll << 32)
+#define KV_TRY "try_wait"
+#else   // (a test builds with less, and a try may take longer than that)
+#define KV_TRY "test_wait"
+#endif
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
-      "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      "{\n\t.reg .pred p;\n\tmbarrier." KV_TRY ".parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
       : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
 // A wait ends after 2^32 clocks (two seconds) at the latest: then the CTA gives
-// up, and every later wait returns at once.
+// up.  Every later wait returns at once, so what is left of a run passes with
+// whatever the tiles hold (every address in it comes from the run, which stays).
+// No role takes another run, whose slot may hold none, and no load is issued for a
+// stage that was not given back, whose barrier may still count a load.
 __device__ __noinline__ void mbar_lost(volatile int* lost, int32_t* err) {
   *lost = 1;
   *reinterpret_cast<volatile int32_t*>(err) = 1;
@@ -553,12 +562,16 @@ __device__ __noinline__ void mbar_lost(volatile int* lost, int32_t* err) {
 __device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatile int* lost, int32_t* err) {
   if (mbar_try(bar, parity)) return;
   const long long from = clock64();
-  while (clock64() - from < (1ll << 32)) {
+  while (!*lost) {
+    if (clock64() - from >= KV_WAIT_CLOCKS) {
+      mbar_lost(lost, err);
+      return;
+    }
     if (mbar_try(bar, parity)) return;
-    if (*lost) return;
   }
-  mbar_lost(lost, err);
 }
+// By a whole warp: whether the CTA has given up, the same for all lanes.
+__device__ __forceinline__ bool gave_up(volatile int* lost) { return __any_sync(~0u, *lost); }
 
 __device__ __forceinline__ bool elect_one() {
   uint32_t r;
@@ -1121,7 +1134,7 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
     if (warp == 10) {
       // ---------------- runs
       Walk w(p, *start, a.c.n_kv_heads);
-      for (uint32_t k = 0; !*lost; k++) {
+      for (uint32_t k = 0;; k++) {
         w.next();
         // the lane's page: stream lane / 16, its tile (lane / 8) % 2
         const int s = lane >> 4, i = (lane >> 3) & 1;
@@ -1132,6 +1145,7 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
           id = a.b.table[(int64_t)g.job.row * a.b.table_stride + pg];
         if (id < 0 || id >= a.c.n_blocks) id = (int)a.c.n_blocks;   // reads as zeros
         if (k >= NR) mbar_wait(REMPTY + 8 * (k % NR), (k / NR - 1) & 1, lost, p.err);
+        if (gave_up(lost)) break;
         Run* const r = runs + k % NR;
         r->page[lane] = id;
         if (lane == 0) {
@@ -1149,13 +1163,13 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
     } else if (warp == 9) {
       // ---------------- loads (the warp as one; one thread issues)
       uint32_t qn = 0, x = 0;   // Q slots used, tiles loaded
-      for (uint32_t k = 0; !*lost; k++) {
+      bool stop = false;
+      for (uint32_t k = 0;; k++) {
         mbar_wait(RFULL + 8 * (k % NR), (k / NR) & 1, lost, p.err);
         const Run& r = runs[k % NR];
-        const int kind = r.kind;
-        if (kind == RUN_END) break;
+        const int kind = r.kind, n0 = r.n[0], n1 = kind == RUN_WIDE ? 0 : r.n[1];
+        if (gave_up(lost) || kind == RUN_END) break;
         if (kind != RUN_NONE) {
-          const int n0 = r.n[0], n1 = kind == RUN_WIDE ? 0 : r.n[1];
           const bool split = kind == RUN_SPLIT;
           // the lane's page of two tiles of its stream (lanes 16 to 31: stream 1), now, next and before
           const Seg& g = r.seg[kind == RUN_PAIR ? lane >> 4 : 0];
@@ -1187,7 +1201,10 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
             int id[TK / 16];
 #pragma unroll
             for (int q = 0; q < TK / 16; q++) id[q] = __shfl_sync(~0u, from, s * 16 + (i & 1) * 8 + q);
-            if (use > 0) mbar_wait(EMPTY + 8 * st, (use - 1) & 1, lost, p.err);
+            if (use > 0) {
+              mbar_wait(EMPTY + 8 * st, (use - 1) & 1, lost, p.err);
+              if ((stop = gave_up(lost))) break;
+            }
             const int head = gs.head;
             if (elect_one()) {
               const CUtensorMap* m = v ? &mv : &mk;
@@ -1204,7 +1221,10 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
             if (u == 1 || (u == 3 && kind == RUN_PAIR)) {   // the rows, after the first K
               for (int o = 0; o < (kind == RUN_WIDE ? 2 : 1); o++) {
                 const uint32_t slot = qn & 1, quse = qn >> 1;
-                if (quse > 0) mbar_wait(QEMPTY + 8 * slot, (quse - 1) & 1, lost, p.err);
+                if (quse > 0) {
+                  mbar_wait(QEMPTY + 8 * slot, (quse - 1) & 1, lost, p.err);
+                  if ((stop = gave_up(lost))) break;
+                }
                 const bool one = gs.job.ntok == 1;
                 const int tok = gs.job.tok0 + o * p.tpt;
                 if (elect_one()) {
@@ -1217,9 +1237,11 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
                 __syncwarp();
                 qn++;
               }
+              if (stop) break;
             }
           }
         }
+        if (stop) break;
         __syncwarp();
         if (lane == 0) mbar_arrive(REMPTY + 8 * (k % NR));
       }
@@ -1238,10 +1260,10 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
         x++;
         return st;
       };
-      for (uint32_t k = 0; !*lost; k++) {
+      for (uint32_t k = 0;; k++) {
         mbar_wait(RFULL + 8 * (k % NR), (k / NR) & 1, lost, p.err);
         const int kind = runs[k % NR].kind, n0 = runs[k % NR].n[0], n1 = runs[k % NR].n[1];
-        __syncwarp();
+        if (gave_up(lost)) break;
         if (lane == 0) mbar_arrive(REMPTY + 8 * (k % NR));
         if (kind == RUN_END) break;
         if (kind == RUN_NONE) continue;
@@ -1312,7 +1334,7 @@ k_kv_attend(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUte
       mbar_wait(RFULL + 8 * (k % NR), (k / NR) & 1, lost, p.err);
       const Run& run = runs[k % NR];
       const int kind = run.kind;
-      if (kind == RUN_END || *lost) break;
+      if (gave_up(lost) || kind == RUN_END) break;
       const bool wide = kind == RUN_WIDE, split = kind == RUN_SPLIT;
       const Seg& g = run.seg[kind == RUN_PAIR ? s : 0];
       const KvJob& job = g.job;
