@@ -545,11 +545,18 @@ rs_status kv_append(rs_ctx* ctx, const rs_kv_cache* cache, const void* k_dev, co
  * A q that is not finite leaves its own row of out and lse unspecified (NaN as
  * a rule) and no other.
  * RS_ERR_TIMEOUT: a kernel of an earlier call gave up on a bounded wait (its
- * outputs are unspecified); reported once, without doing this call's work. */
+ * outputs are unspecified); reported once, without doing this call's work.  A
+ * replayed call is not looked at like this: kv_status is. */
 rs_status kv_attend(rs_ctx* ctx, const rs_kv_cache* cache, const rs_kv_batch* batch,
                     const void* q_dev, int32_t n_heads, int64_t q_token_stride,
                     int64_t q_head_stride, float scale, void* out_dev, int64_t out_token_stride,
                     int64_t out_head_stride, float* lse_dev);
+
+/* RS_ERR_TIMEOUT, once, if a kv_attend of this context gave up on a bounded wait
+ * since the last report, in a call or in a replay of a captured one; RS_OK if
+ * none did.  Synchronises with the context's stream; replays on other streams
+ * have to have ended.  RS_ERR_STATE while the stream is being captured. */
+rs_status kv_status(rs_ctx* ctx);
 
 #ifdef __cplusplus
 }

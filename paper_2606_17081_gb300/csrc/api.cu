@@ -1417,6 +1417,25 @@ rs_status kv_append(rs_ctx* ctx, const rs_kv_cache* cache, const void* k_dev, co
   return RS_OK;
 }
 
+// Whether a kv_attend that has ended gave up; each is reported once.
+static rs_status kv_gave_up(rs_ctx* ctx) {
+  volatile int32_t* const err = ctx->kv_err;
+  if (!err || !*err) return RS_OK;
+  *err = 0;
+  return fail(ctx, RS_ERR_TIMEOUT, "an earlier kv_attend gave up waiting for its own copies or products");
+}
+
+rs_status kv_status(rs_ctx* ctx) {
+  if (!ctx) return fail(nullptr, RS_ERR_INVALID, "ctx is NULL");
+  ctx->err.clear();
+  cudaStreamCaptureStatus capture;
+  CK(cudaStreamIsCapturing(ctx->st, &capture), "cudaStreamIsCapturing");
+  if (capture != cudaStreamCaptureStatusNone)
+    return fail(ctx, RS_ERR_STATE, "the stream is being captured");
+  CK(cudaStreamSynchronize(ctx->st), "cudaStreamSynchronize");
+  return kv_gave_up(ctx);
+}
+
 rs_status kv_attend(rs_ctx* ctx, const rs_kv_cache* cache, const rs_kv_batch* batch,
                     const void* q_dev, int32_t n_heads, int64_t q_token_stride,
                     int64_t q_head_stride, float scale, void* out_dev, int64_t out_token_stride,
@@ -1467,10 +1486,7 @@ rs_status kv_attend(rs_ctx* ctx, const rs_kv_cache* cache, const rs_kv_batch* ba
     CK(cudaMallocHost(reinterpret_cast<void**>(&ctx->kv_err), sizeof(int32_t)), "cudaMallocHost");
     *ctx->kv_err = 0;
   }
-  if (*static_cast<volatile int32_t*>(ctx->kv_err)) {
-    *ctx->kv_err = 0;
-    return fail(ctx, RS_ERR_TIMEOUT, "an earlier kv_attend gave up waiting for its own copies or products");
-  }
+  if ((r = kv_gave_up(ctx)) != RS_OK) return r;
   if ((r = ensure(ctx, ctx->kv_ws, need, "attention workspace")) != RS_OK) return r;
   CK(launch_kv_attend(a, ctx->kv_ws.p, ctx->kv_err, ctx->sms, ctx->st), "attention launch");
   return RS_OK;

@@ -107,7 +107,8 @@ class rs_kv_batch(C.Structure):
 EXPORTS = ["rs_config_default", "route_init", "route_destroy", "route_last_error",
            "route_hash_blocks", "route_dup_flags", "route_batch", "route_probe", "route_release", "route_active",
            "simulate_replicas", "poa_estimate", "route_cache_dump", "route_last_timing",
-           "poa_estimate_noalloc", "sweep_knee", "kv_tables", "kv_append", "kv_attend"]
+           "poa_estimate_noalloc", "sweep_knee", "kv_tables", "kv_append", "kv_attend",
+           "kv_status"]
 
 _lib = None
 
@@ -153,6 +154,7 @@ def lib():
             "kv_append": (i32, [vp, C.POINTER(rs_kv_cache), vp, vp, i64, i64, i32, vp]),
             "kv_attend": (i32, [vp, C.POINTER(rs_kv_cache), C.POINTER(rs_kv_batch), vp, i32, i64,
                                 i64, C.c_float, vp, i64, i64, vp]),
+            "kv_status": (i32, [vp]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)
@@ -431,6 +433,11 @@ def kv_attend(ctx, cache: KVCache, batch: KVBatch, q, scale: float, out, lse=Non
                                    out.data_ptr(), os[0], os[1], lp)
     if st:
         _check(st, ctx)
+
+
+def kv_status(ctx) -> None:
+    """Raises RS_ERR_TIMEOUT if a kv_attend, called or replayed, gave up on a bounded wait since the last report."""
+    _check(lib().kv_status(ctx), ctx)
 
 
 # ----------------------------------------------------------------- marshalling helpers

@@ -76,3 +76,48 @@ def test_a_call_that_gives_up_ends_and_is_reported(tmp_path, clocks):
     assert r.returncode == 0, r.stdout + r.stderr
     if clocks == 0:
         assert r.stdout.split("GAVE UP")[1].split() == ["True"] * 3, r.stdout
+
+
+REPLAYED = r"""
+import sys
+sys.path[:0] = [sys.argv[1], sys.argv[1] + "/tests"]
+import torch
+from kv_reference import Step
+from paper_2606_17081_gb300 import routesim as rs
+usual = rs.LIB_PATH
+for lib in (sys.argv[2], usual):
+    rs.LIB_PATH, rs._lib = lib, None
+    st = torch.cuda.Stream()
+    ctx = rs.Context(W=1, K=1024, stream=st.cuda_stream)
+    rs.kv_status(ctx.h)
+    s = Step(0, [1], [700], 8, 2, 128, torch.bfloat16)
+    cache, batch, q = s.to(rs)
+    out = torch.zeros_like(q)
+    torch.cuda.synchronize()
+    def status():
+        try:
+            rs.kv_status(ctx.h)
+        except rs.RoutesimError as e:
+            return e.status
+        return 0
+    rs.kv_attend(ctx.h, cache, batch, q, s.scale, out)
+    gives_up = rs.RS_ERR_TIMEOUT if lib != usual else 0
+    assert [status(), status()] == [gives_up, 0]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=st):
+        rs.kv_attend(ctx.h, cache, batch, q, s.scale, out)
+        assert status() == rs.RS_ERR_STATE
+    assert status() == 0
+    with torch.cuda.stream(st):
+        g.replay()
+        g.replay()
+    assert [status(), status()] == [gives_up, 0]
+    ctx.close()
+print("REPORTED")
+"""
+
+
+def test_a_replay_that_gives_up_is_reported(tmp_path):
+    lib = built_with(0, tmp_path)
+    r = subprocess.run([sys.executable, "-c", REPLAYED, ROOT, lib], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and "REPORTED" in r.stdout, r.stdout + r.stderr

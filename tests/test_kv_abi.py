@@ -51,3 +51,10 @@ def test_descriptors_refuse_host_tensors():
     i = torch.zeros(1, dtype=torch.int32)
     with pytest.raises(rs.RoutesimError, match="GPU"):
         rs.KVBatch(i[None], i, i, 1)
+
+
+def test_status_refuses_a_null_context():
+    B.build()
+    assert rs.lib().kv_status(None) == rs.RS_ERR_INVALID
+    with pytest.raises(rs.RoutesimError, match="NULL"):
+        rs.kv_status(None)
