@@ -1357,7 +1357,7 @@ static rs_status check_cache(rs_ctx* ctx, const rs_kv_cache* c, rs_kv_cache* out
 
 static rs_status check_batch(rs_ctx* ctx, const rs_kv_batch* b) {
   if (!b) return fail(ctx, RS_ERR_INVALID, "batch is NULL");
-  if (b->n_req < 0 || b->n_req > 16384)
+  if (b->n_req < 0 || b->n_req > KV_MAX_REQ)
     return fail(ctx, RS_ERR_INVALID, "n_req must be in [0, 16384]");
   if (b->n_tokens < 0 || b->n_tokens > (1 << 24))
     return fail(ctx, RS_ERR_INVALID, "n_tokens must be in [0, 2^24]");

@@ -221,7 +221,9 @@ cudaError_t launch_kv_tables(const rs_kv_batch& b, const int32_t* q_len, const i
                              const int32_t* free_ids, int64_t n_free, int32_t* positions,
                              int64_t* slots, int64_t* counts, int sms, cudaStream_t st) {
   const size_t smem = ((size_t)2 * b.n_req + (b.n_groups <= TAB_GROUPS ? b.n_groups + 1 : 0)) * 4;
-  cudaError_t e = cudaFuncSetAttribute(k_kv_tables, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  // (the limit belongs to the kernel, not to the call: every call sets the most that any needs, or another thread's call
+  // could lower it before this one's launch)
+  cudaError_t e = cudaFuncSetAttribute(k_kv_tables, cudaFuncAttributeMaxDynamicSharedMemorySize, (2 * KV_MAX_REQ + TAB_GROUPS + 1) * 4);
   if (e != cudaSuccess) return e;
   // rows in threads and requests in warps
   const int64_t want = std::max<int64_t>((b.n_tokens + NT_TAB - 1) / NT_TAB, (b.n_req + 15) / 16);

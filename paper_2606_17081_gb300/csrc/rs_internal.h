@@ -299,6 +299,7 @@ cudaError_t launch_behind(Kernel k, unsigned grid, unsigned threads, size_t smem
   return cudaLaunchKernelEx(&c, k, args...);
 }
 #endif
+constexpr int KV_MAX_REQ = 16384;   // requests of a step
 cudaError_t launch_kv_tables(const rs_kv_batch& b, const int32_t* q_len, const int32_t* prev_len,
                              const int32_t* prefix_blocks, int64_t prefix_stride,
                              const int32_t* free_ids, int64_t n_free, int32_t* positions,
