@@ -319,7 +319,7 @@ cudaError_t launch_dup_flags(const HashJob* jobs_dev, int njobs, int64_t total_r
   int wpc = (int)std::min<size_t>(8, std::max<size_t>(1, dflt / per_warp));
   const size_t smem = per_warp * wpc;
   if (smem > dflt) {
-    e = cudaFuncSetAttribute(k_dup_flags, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    e = allow_smem(k_dup_flags);
     if (e != cudaSuccess) return e;
   }
   int64_t nblk = (total_req + wpc - 1) / wpc;

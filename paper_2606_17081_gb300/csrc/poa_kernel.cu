@@ -1390,9 +1390,7 @@ cudaError_t launch_poa(const PoaProblem* d_prob, int nprob, const PoaBuffers& b,
     kern = mc.W == 3 ? k_poa_solve<3, 1>
                      : (mc.W == 6 ? k_poa_solve<6, 1> : k_poa_solve<POA_WMAX, 1>);
   const size_t smem = wide ? poa_wide_smem(mc.W) : 0;
-  if (wide && (e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                        (int)smem)) != cudaSuccess)
-    return e;
+  if (wide && (e = allow_smem(kern)) != cudaSuccess) return e;
   const int nt = wide ? NT_WIDE : (few ? 32 * NW_SOLVE : NT_SOLVE);
   const int wpc = wide || few ? 1 : NT_SOLVE / 32;   // windows of a CTA
   if (b.wnext) {

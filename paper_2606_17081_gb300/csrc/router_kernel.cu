@@ -272,8 +272,7 @@ cudaError_t launch_route_batch(const RouterState& s, int32_t instance, const int
                                float tau, uint64_t seed, bool lean, cudaStream_t st) {
   if (n_req <= 0) return cudaSuccess;
   const size_t smem = router_smem(mc.W, nbmax, lean);
-  cudaError_t e = cudaFuncSetAttribute(k_route_batch, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       (int)smem);
+  const cudaError_t e = allow_smem(k_route_batch);
   if (e != cudaSuccess) return e;
   SimBuffers b{};
   b.keys = s.keys;

@@ -275,6 +275,20 @@ cudaError_t launch_route_release(const RouterState& s, const int32_t* worker, co
 cudaError_t launch_clear_tables(uint64_t* keys, uint32_t* stamp, size_t nslots, CacheMeta* meta,
                                 size_t nmeta, cudaStream_t st);
 
+// Lets a kernel's launches have all the dynamic shared memory that fits beside its
+// static.  The limit belongs to the kernel, not to a launch: set to one launch's
+// size, it could be lowered by another thread's context before that launch.
+template <class Kernel>
+cudaError_t allow_smem(Kernel k) {
+  int dev = 0, most = 0;
+  cudaFuncAttributes f;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev);
+  if (e == cudaSuccess) e = cudaFuncGetAttributes(&f, k);
+  if (e != cudaSuccess) return e;
+  return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, most - (int)f.sharedSizeBytes);
+}
+
 // A worker's paged KV cache (arguments checked by the caller).  These kernels
 // follow one another in a step, so each may begin before the one ahead of it in
 // the stream has ended: it waits (behind_stream) before it touches memory, and it

@@ -2573,7 +2573,7 @@ cudaError_t launch_sim_ids(const SimDesc* d_desc, const SimBuffers& b, const Sim
     kern = var == 0 ? (sg ? k_sim_ids<2, 5, true, 0> : k_sim_ids<2, 5, false, 0>)
                     : (sg ? k_sim_ids<2, 5, true, 2>
                           : (var == 1 ? k_sim_ids<2, 5, false, 1> : k_sim_ids<2, 5, false, 2>));
-  e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  e = allow_smem(kern);
   if (e != cudaSuccess) return e;
   kern<<<L.nsim, (nu + 2) * 32, smem, st>>>(d_desc, b, L);
   return cudaGetLastError();

@@ -932,7 +932,7 @@ cudaError_t launch_sim(const SimDesc* d_desc, const SimBuffers& b, const SimLaun
   else
     kern = one ? (L.slots_global ? k_sim<1, true, SIM_LRU> : k_sim<1, false, SIM_LRU>)
                : (L.slots_global ? k_sim<2, true, SIM_LRU> : k_sim<2, false, SIM_LRU>);
-  e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  e = allow_smem(kern);
   if (e != cudaSuccess) return e;
   kern<<<L.nsim, NT_SIM, smem, st>>>(d_desc, b, L);
   return cudaGetLastError();
