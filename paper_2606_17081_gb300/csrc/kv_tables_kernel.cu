@@ -51,11 +51,11 @@ __device__ __forceinline__ Lens req_lens(const int32_t* q_len, const int32_t* pr
 // Bound: launch and latency.  64 requests of single tokens (26 KB): 4.7 us; 1024
 // prompts with 262 000 tokens (3.8 MB, 0.6 us at the copy rate): 11.6 us, of which
 // a row's search and lengths are most.
-__global__ void __launch_bounds__(NT_TAB) k_kv_tables(rs_kv_batch b, const int32_t* __restrict__ q_len,
-                                                      const int32_t* __restrict__ prev_len,
-                                                      const int32_t* __restrict__ prefix_blocks,
-                                                      int64_t prefix_stride,
-                                                      const int32_t* __restrict__ free_ids, int64_t n_free,
+// The inputs are not __restrict__, here and below: such reads may go by the read-only path, which asks for data that
+// nobody writes while the kernel runs, and it runs already (behind_stream) while the kernel before it writes.
+__global__ void __launch_bounds__(NT_TAB) k_kv_tables(rs_kv_batch b, const int32_t* q_len, const int32_t* prev_len,
+                                                      const int32_t* prefix_blocks, int64_t prefix_stride,
+                                                      const int32_t* free_ids, int64_t n_free,
                                                       int32_t* __restrict__ positions,
                                                       int64_t* __restrict__ slots,
                                                       int64_t* __restrict__ counts) {
@@ -183,9 +183,8 @@ __global__ void __launch_bounds__(NT_TAB) k_kv_tables(rs_kv_batch b, const int32
 // heads of 128): 18.4 us, 7.1 TB/s; 20.2 us with loads through L1, 22.0 us
 // with 64-bit places too, 24.5 us with UNR = 8.
 template <class T, int UNR>
-__global__ void __launch_bounds__(256) k_kv_append(rs_kv_cache c, const uint16_t* __restrict__ k,
-                                                   const uint16_t* __restrict__ v, int64_t ts, int64_t hs,
-                                                   uint32_t total, const int64_t* __restrict__ slots,
+__global__ void __launch_bounds__(256) k_kv_append(rs_kv_cache c, const uint16_t* k, const uint16_t* v,
+                                                   int64_t ts, int64_t hs, uint32_t total, const int64_t* slots,
                                                    uint32_t row_pieces, uint32_t head_pieces) {
   constexpr int V = sizeof(T) / 2;
   const int64_t end = c.n_blocks * 16;
