@@ -439,6 +439,9 @@ rs_status poa_estimate_noalloc(const rs_config* cfg, const rs_records* records, 
  * them (kv_attend).  The paper assumes a serving engine here and gives no
  * kernels; layouts and rules below are this library's.
  *
+ * Of the context these calls use the stream, and kv_attend a workspace and a flag;
+ * W, the cache sizes and the instances of route_init play no part in them.
+ *
  * A step: n_req requests, request i with q_len[i] >= 0 new tokens after
  * prev_len[i] cached ones, kv_len[i] = prev_len[i] + q_len[i].  The tokens of
  * request i are rows q_start[i] .. q_start[i+1] - 1 of every per-token array;
@@ -447,7 +450,8 @@ rs_status poa_estimate_noalloc(const rs_config* cfg, const rs_records* records, 
  * + t.  All calls are asynchronous on the context stream, read lengths and
  * tables on the device only, and neither read nor write outside the arrays
  * described here, whatever the lengths and tables hold.  The workspace of
- * kv_attend grows at a call larger than those before it (cudaMalloc), so a
+ * kv_attend (some 20 to 40 MB, and with groups 2 n_tokens n_heads (4 head_dim +
+ * 8) bytes more) grows at a call larger than those before it (cudaMalloc), so a
  * stream capture follows one such call outside it (else RS_ERR_STATE, without
  * a launch); what a capture holds stays until route_destroy, and is shared:
  * replays and calls of one context must not overlap on the GPU. */

@@ -16,11 +16,12 @@
 // cut by a share's end leave parts in 32 bits.
 //
 // What bounds it (one GB300): single tokens over long contexts, HBM (256 requests
-// of 256 to 8192 own tokens, 8 kv heads of 128: 2.4 GB in 358 us, 6.7 TB/s); prompts
-// and prefixes that many rows share, the tensor cores (4096 tokens behind 12 288,
-// 32 heads: 634 us, 1.52 PFLOP/s, 128 keys for 256 rows in 1.3 us of which the
-// products alone take 1.05); short steps, the chain plan - loads - product - softmax -
-// product - stores - join (one token over 701 keys: 14 us).
+// in 8 groups, 256 to 8192 own tokens each, 8 kv heads of 128: 2.6 GB in 418 us, 6.3
+// TB/s); prompts and prefixes that many rows share, the tensor cores (4096 tokens
+// behind 12 288, 32 heads: 645 us, 1.49 PFLOP/s; 128 keys for 256 rows take 2048
+// clocks of the products and, with all that is between tiles and jobs, 2955 of the
+// kernel's); short steps, the chain plan - loads - product - softmax - product -
+// stores - join (one token over 701 keys: 14 us).
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -37,11 +38,12 @@ namespace {
 
 constexpr int TK = 128;        // keys of a tile
 // Costs, in quarters of a microsecond or so: a tile of a job of at most 128 rows,
-// one of a larger job, and a job's own (its rows' loads and stores).  A wide tile
-// takes 1.3 us, a narrow one 0.8 us from L2 and 1.4 us where all SMs wait for HBM.
+// one of a larger job, and a job's own (its rows' loads and stores).  They share the
+// work out and are fitted to that, not measured one by one.  When they were chosen
 // 64 requests on a prefix of 32 768, 8 groups of 256 in all, 6 prompts of 100 to
-// 2047 on a prefix: 83, 427, 259 us; with 4, 6, 3, 10: 86, 427, 273 us; with equal
-// tiles and OV 2 for all, on an earlier kernel: 142, 524, 299 us.
+// 2047 on a prefix took 83, 427, 259 us; with 4, 6, 3, 10: 86, 427, 273 us; with
+// equal tiles and OV 2 for all, on an earlier kernel: 142, 524, 299 us (now 84, 418,
+// 254).
 constexpr int W_NARROW = 4, W_WIDE = 5, OV_NARROW = 3, OV_WIDE = 10;
 constexpr int NT_PLAN = 1024;
 constexpr int NT_ATT = 384;
@@ -1704,7 +1706,7 @@ cudaError_t run(const KvAttendArgs& a, const KvPlan& p, const CUtensorMap* m, cu
   const int64_t rows = std::min<int64_t>((int64_t)p.ctas * 256, (int64_t)a.b.n_tokens * a.n_heads) +
                        (a.b.n_groups ? (int64_t)a.b.n_tokens * a.n_heads : 0);
   // Few rows: eight parts of each on their way at once (111 registers, 16 rows an SM); many: four (75 registers, 24 rows).
-  // Eight and four, us a call in a replayed graph: 256 tokens x heads behind a prefix 17.9 and 18.2, 924 23.6 and 24.1,
+  // Eight and four, us a call in a replayed graph, when it was chosen: 256 tokens x heads behind a prefix 17.9 and 18.2, 924 23.6 and 24.1,
   // 4096 85.1 and 84.4, 8192 411 and 408, 6 prompts' 200 000 263 and 256
   auto join = rows < (int64_t)p.ctas * 48 ? k_kv_join<D, HALF, 8> : k_kv_join<D, HALF, 4>;
   return launch_behind(join, (unsigned)std::min<int64_t>((rows + 7) / 8, (int64_t)p.ctas * 8), 256, 0, st, a, p);
