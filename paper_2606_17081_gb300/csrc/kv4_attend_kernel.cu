@@ -173,7 +173,7 @@ __device__ __forceinline__ void tiny_plan(const rs_kv_batch& b, const Plan& p, H
   const int n = b.n_req, G = b.n_groups, max_keys = max_keys_of(b);
   Lens r{0, 0, 0};
   if (lane < n) r = lens_of(b, lane);
-  const int q_end = n > 0 ? clampi(b.q_start[n], 0, b.n_tokens) : 0;
+  const int q_begin = n > 0 ? clampi(b.q_start[0], 0, b.n_tokens) : 0, q_end = n > 0 ? clampi(b.q_start[n], 0, b.n_tokens) : 0;
   // lane g: the group's requests, its rows, and its prefix
   int g0 = 0, g1 = 0, T0 = 0, T1 = 0, P = 0;
   if (lane < G) {
@@ -276,6 +276,7 @@ __device__ __forceinline__ void tiny_plan(const rs_kv_batch& b, const Plan& p, H
     h.total[0] = all * p.chunks;
     h.per[0] = share_of(h.total[0], p.workers[0], 0);
     h.ctas = p.workers[1];
+    h.q_begin = q_begin;
     h.q_end = q_end;
     h.room = 1;
     *head = h;
@@ -319,7 +320,7 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv4_plan(rs_kv_batch b, Plan p, int
   // what every later step goes by, on its way at once
   Lens mine{0, 0, 0};
   if (tid < n) mine = lens(tid);
-  const int q_end = n > 0 ? rows_at(n) : 0;
+  const int q_begin = n > 0 ? rows_at(0) : 0, q_end = n > 0 ? rows_at(n) : 0;
   const int g_lo = G > 0 ? b.group_start[0] : 0, g_hi = G > 0 ? b.group_start[G] : 0;
   if (G > 0) {
     if (staged)
@@ -511,6 +512,7 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv4_plan(rs_kv_batch b, Plan p, int
       h.total[1] = before.c1 * heads;
     }
     split(p, h, (int64_t)h.jobs[1] * heads, s_longest, d128);
+    h.q_begin = q_begin;
     h.q_end = q_end;
     h.room = room;
     *p.head = h;
@@ -938,10 +940,12 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_kv4_rows(const __grid_constan
     }
   }
   // rows of no request
-  const int q_end = head->q_end;
-  const int64_t per = (int64_t)a.n_heads * (D / 8), pads = (a.b.n_tokens - q_end) * per;
+  const int q_begin = head->q_begin, q_end = head->q_end;
+  const int64_t per = (int64_t)a.n_heads * (D / 8), pads = (int64_t)(q_begin + a.b.n_tokens - q_end) * per;
   for (int64_t x = (int64_t)blockIdx.x * (WARPS * 32) + tid; x < pads; x += (int64_t)gridDim.x * (WARPS * 32)) {
-    const int64_t r = x / per + q_end, y = x % per, h = y / (D / 8), e = y % (D / 8);
+    const int64_t y = x % per, h = y / (D / 8), e = y % (D / 8);
+    int64_t r = x / per;
+    if (r >= q_begin) r += q_end - q_begin;
     reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + r * a.o_ts + h * a.o_hs)[e] = make_uint4(0, 0, 0, 0);
     if (a.lse && e == 0) a.lse[r * a.n_heads + h] = -INFINITY;
   }
@@ -980,8 +984,9 @@ struct Parts {
         const int at = w & (KIND - 1), workers = kind[s] ? p.workers[1] : p.workers[0];
         const int4 v = at < workers ? __ldcg(reinterpret_cast<const int4*>((kind[s] ? p.cut[1] : p.cut[0]) + at)) : make_int4(0, -1, 0, 0);
         const int64_t r = (tok - v.w) * p.ratio + hl - v.z;
-        // (starts that decrease leave rows of which nothing was written: they may find anything)
-        const bool sound = v.x >= 0 && v.x <= v.y && v.y < workers && r >= 0 && r < rows_of(kind[s]);
+        // (starts that decrease leave rows of which nothing was written: they may find anything, also a CTA's part in a
+        // step that has no room for any)
+        const bool sound = (!kind[s] || p.cap[1] > 0) && v.x >= 0 && v.x <= v.y && v.y < workers && r >= 0 && r < rows_of(kind[s]);
         count[s] = sound ? v.y - v.x + 1 : 0;
         first[s] = v.x;
         row[s] = sound ? (int)r : 0;
@@ -1098,10 +1103,10 @@ __device__ __forceinline__ void join_parts(const KvAttend4Args& a, const Plan& p
 // Bound: latency, of reads that depend on one another (head, place, cut, sums, rows): 3 to 6 us.  Three CTAs an SM and four
 // rows on their way (four CTAs: 0 to 2 us more, six to eight: up to 8 us more; eight rows: up to 4 us more).
 template <int D, bool HALF>
-__device__ __forceinline__ void join_by_cta(const KvAttend4Args& a, const Plan& p, int64_t rows, float (*sm)[D + 4]) {
+__device__ __forceinline__ void join_by_cta(const KvAttend4Args& a, const Plan& p, int64_t from, int64_t rows, float (*sm)[D + 4]) {
   constexpr int C = D / 32;
   const int j = threadIdx.x & 7, eight = threadIdx.x >> 3;
-  for (int64_t home = blockIdx.x; home < rows; home += gridDim.x) {
+  for (int64_t home = from + blockIdx.x; home < rows; home += gridDim.x) {
     const Parts q(a, p, home);
     if (!q.any) continue;
     const int64_t tok = quotient(home, a.n_heads);
@@ -1127,12 +1132,12 @@ __device__ __forceinline__ void join_by_cta(const KvAttend4Args& a, const Plan& 
 
 // A lane has D / 32 elements of the row; a lane a part's sums, up to 32 parts at once, the rows four at a time.
 template <int D, bool HALF>
-__device__ __forceinline__ void join_by_warp(const KvAttend4Args& a, const Plan& p, int64_t rows) {
+__device__ __forceinline__ void join_by_warp(const KvAttend4Args& a, const Plan& p, int64_t from, int64_t rows) {
   constexpr int E = D / 32, Z = 4;
   using Vec = std::conditional_t<E == 4, float4, float2>;
   const int lane = threadIdx.x & 31;
   const int64_t warps = (int64_t)gridDim.x * 8, me = (int64_t)(threadIdx.x >> 5) * gridDim.x + blockIdx.x;
-  for (int64_t base = me; base < rows; base += 32 * warps) {
+  for (int64_t base = from + me; base < rows; base += 32 * warps) {
     const int64_t mine = base + lane * warps;
     const Parts own(a, p, min(mine, rows - 1));
     for (unsigned todo = __ballot_sync(~0u, own.any && mine < rows); todo; todo &= todo - 1) {
@@ -1206,9 +1211,9 @@ __global__ void __launch_bounds__(256, JOINS) k_kv4_join(const __grid_constant__
   __shared__ float sm[32][D + 4];
   behind_stream();
   const int q_end = p.head->room ? p.head->q_end : 0;
-  const int64_t rows = (int64_t)q_end * a.n_heads;
-  if (ONE || rows <= 16 / JOINS * (int64_t)gridDim.x) join_by_cta<D, HALF>(a, p, rows, sm);
-  else join_by_warp<D, HALF>(a, p, rows);
+  const int64_t from = (int64_t)p.head->q_begin * a.n_heads, rows = (int64_t)q_end * a.n_heads;   // the first, the end
+  if (ONE || rows <= 16 / JOINS * (int64_t)gridDim.x) join_by_cta<D, HALF>(a, p, from, rows, sm);
+  else join_by_warp<D, HALF>(a, p, from, rows);
 }
 
 // ------------------------------------------------------------------ host

@@ -54,11 +54,12 @@ struct Head {
   int64_t total[2];     // cost of all items of a kind
   int64_t per[2];       // of a worker's share
   int32_t jobs[2];
-  int32_t q_end;        // rows from here on belong to no request
+  int32_t q_begin;      // rows before this belong to no request,
+  int32_t q_end;        // and rows from here on
   int32_t room;         // the jobs had room
   int32_t whole;        // a CTA has an item and no more (short ones: no cuts, nothing to join)
   int32_t ctas;         // of the warps' kernel that have work
-  int32_t reserved[2];
+  int32_t reserved0;
 };
 
 constexpr int TOK_ALONE = 0, TOK_BOTH = 1, TOK_PREFIX = 2;   // a token's rows have an own job, both, a prefix job
