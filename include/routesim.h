@@ -607,7 +607,8 @@ rs_status kv_read4(rs_ctx* ctx, const rs_kv_cache4* cache, const int64_t* slots_
  * statistics and sums are in 32 bits, the weights p_j are rounded once to 11 significant bits for
  * the product with V (weights below 2^-27 of their row's largest may lose more, or all), and out
  * once at the end.  A q in bf16 enters as it is, except elements below 2^-30 of their row's largest,
- * which are rounded to 2^-38 of that. */
+ * which are rounded to 2^-38 of that.  Any scale that is finite and > 0 will do; where scores are past
+ * 2^127 in size, lse is unspecified. */
 rs_status kv_attend4(rs_ctx* ctx, const rs_kv_cache4* cache, const rs_kv_batch* batch, int32_t dtype,
                      const void* q_dev, int32_t n_heads, int64_t q_token_stride,
                      int64_t q_head_stride, float scale, void* out_dev, int64_t out_token_stride,

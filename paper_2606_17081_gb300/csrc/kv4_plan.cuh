@@ -260,9 +260,13 @@ __device__ __forceinline__ float log_sum(float m, float l, float sl) {
   return l > 0.0f ? __fmul_rn(__fadd_rn(__fmul_rn(m, sl), __fsub_rn(__log2f(l), BIAS)), LN2) : l == l ? -INFINITY : l;
 }
 
-// What a row's scores are multiplied by, in powers of two (never 0: a hidden score is -inf).
+// What a row's scores are multiplied by, in powers of two (never 0: a hidden score is -inf).  The row's power comes first:
+// a small scale and a large q, or the other way round, meet before bits can be lost.  Past the largest number it ends
+// there: scores are 2^-34 apart or equal, so any two that differ are as far apart as weights tell, and equal ones stay equal.
 __device__ __forceinline__ float row_factor(const KvAttend4Args& a, float inverse) {
-  return fmaxf(__fmul_rn(__fmul_rn(__fmul_rn(a.scale, LOG2E), a.c.k_unit), inverse), 1.17549435e-38f);
+  constexpr float MOST = 3.402823466e38f;
+  const float f = fminf(__fmul_rn(__fmul_rn(a.scale, inverse), LOG2E), MOST);
+  return fminf(fmaxf(__fmul_rn(f, a.c.k_unit), 1.17549435e-38f), MOST);
 }
 
 // Keys that token `tok` (of the step) with row's place `in` in its job's request sees of a job, from key 0 on.

@@ -1,0 +1,51 @@
+"""kv_attend4 at the ends of what scales, units and sizes may be.  Bounds as in kv4_reference.compare."""
+import pytest
+
+from kv4_reference import Step4, compare
+from paper_2606_17081_gb300 import routesim as rs
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("needs a CUDA device", allow_module_level=True)
+
+from test_gpu_kv4_attend import BF, HF, attend, ctx  # noqa: E402, F401
+
+STEPS = [([1], [700], None), ([1], [9000], None), ([70], [300], None), ([1] * 6, [260, 300, 256, 290, 400, 257], ([0, 6], [256])), ([3, 1, 200], [0, 40, 500], None)]
+
+
+@pytest.mark.parametrize("new,ctxs,groups", STEPS)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("q_power,k_power,unit_power", [(-124, -6, 24), (122, 10, -24), (0, 0, 0), (-100, 0, 24), (100, 0, -24), (110, -6, 24)])
+def test_scales_that_make_up_for_sizes(ctx, new, ctxs, groups, dim, q_power, k_power, unit_power):  # noqa: F811
+    """Ordinary scores of rows and units of extreme sizes: scale * unit alone may be past 2^128 or below 2^-126."""
+    s = Step4(81, new, ctxs, 4, 2, dim, BF, *(groups or ()), k_unit=2.0 ** unit_power)
+    s.q = (s.q.double() * 2.0 ** q_power).to(BF)
+    s.k *= 2.0 ** k_power
+    s.scale = 1.23 * dim ** -0.5 * 2.0 ** -(q_power + k_power + unit_power)
+    compare(s, *attend(ctx, s))
+
+
+@pytest.mark.parametrize("new,ctxs,groups", STEPS)
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("unit_power", [0, 24])
+def test_the_largest_scale(ctx, new, ctxs, groups, dtype, unit_power):  # noqa: F811
+    """Keys of zeros weigh the same; else all weight is on the keys that score highest."""
+    s = Step4(82, new, ctxs, 4, 2, 64, dtype, *(groups or ()), k_unit=2.0 ** unit_power)
+    empty = s.k.isnan()
+    s.k.zero_()
+    s.k[:, 1, :, 0] = (torch.arange(s.k.shape[0] * 16).view(-1, 16) * 7 % 23 % 5 + 1) * s.k_unit   # (6 has the code of its own)
+    s.k[:, 1, :, 0].clamp_(max=4 * s.k_unit)
+    s.k[empty] = float("nan")
+    s.q[:, 2:] = 0
+    s.q[:, 2:, 0] = 1.0
+    s.scale = 3e38
+    out, lse = attend(ctx, s)
+    s.scale = torch.tensor(s.scale, dtype=torch.float32).item()
+    want, want_lse = s.expected()
+    far = want_lse.clone()
+    far[:, 2:] = torch.where(torch.isinf(far[:, 2:]), far[:, 2:], 0.0)   # (their log sums are past the largest number, and not looked at)
+    lse[:, 2:] = far[:, 2:].to(lse)
+    s.expected = lambda: (want, far)
+    compare(s, out, lse)
