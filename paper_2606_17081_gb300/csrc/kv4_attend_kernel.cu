@@ -164,7 +164,10 @@ __device__ __forceinline__ int64_t few_take(int64_t rows, int keys) {
 // head: from 7 us of all SMs on.  (Work less, and a call with and without, us: 8 requests of 4 rows on 1 024 keys 0.6,
 // 19.8 and 16.6; 98 of 5 on 1 040, one kv head, 1.4, 35.8 and 26.7; 4 of 4 on 16 384 5.1, 30.6 and 27.1; 2 of 4 on 65 536
 // 8.6, 34.7 and 42.1; 40 of 4 on 2 048 9.4, 39.7 and 42.6.)
-__device__ __forceinline__ bool worth(const Plan& p, int64_t saved) { return saved * p.heads >= 700 * (int64_t)p.workers[1]; }
+#ifndef KV4_WORTH   // (a test builds with 0: every prefix is shared that costs less so)
+#define KV4_WORTH 700
+#endif
+__device__ __forceinline__ bool worth(const Plan& p, int64_t saved) { return saved * p.heads >= (int64_t)KV4_WORTH * p.workers[1]; }
 
 // The plan of a step of at most TINY requests, all of few rows, by one warp of every CTA for
 // itself: a lane a request, of at most two jobs, then a group.
