@@ -93,7 +93,7 @@ __device__ __forceinline__ Lens lens_of(const rs_kv_batch& b, int i) {
   r.kv = clampi((int64_t)max(kv, 0) - end + r.q0 + r.q, -(1 << 24), INT_MAX - 1);
   return r;
 }
-__device__ __forceinline__ int units_of(int kind, int keys) { return keys > 0 ? (keys + keys_of(kind) - 1) / keys_of(kind) : 0; }
+__device__ __forceinline__ int units_of(int kind, int keys) { return keys > 0 ? (keys - 1) / keys_of(kind) + 1 : 0; }
 __device__ __forceinline__ int max_keys_of(const rs_kv_batch& b) { return (int)min((int64_t)b.max_blocks * 16, (int64_t)INT_MAX - 256); }
 
 // Job k of request i (its cost's sum left out).

@@ -142,7 +142,7 @@ import pytest
 from paper_2606_17081_gb300 import routesim as rs
 rs.LIB_PATH = sys.argv[2]
 sys.exit(pytest.main(["-x", "-q", "-p", "no:cacheprovider", "-m", "gpu", sys.argv[1] + "/test_gpu_kv4_shared.py", sys.argv[1] + "/test_gpu_kv4_limits.py",
-                      sys.argv[1] + "/test_gpu_kv4_attend.py", "-k", sys.argv[3]]))
+                      sys.argv[1] + "/test_gpu_kv4_lengths.py", sys.argv[1] + "/test_gpu_kv4_attend.py", "-k", sys.argv[3]]))
 """
 
 
@@ -154,7 +154,7 @@ def test_with_every_prefix_shared(tmp_path):
     subprocess.run([B._nvcc(), *B.ARCH, *B.FLAGS, "-DKV4_WORTH=0", "-c", src, "-o", obj], check=True, capture_output=True)
     rest = [os.path.join(B.BUILD, s.replace(".cu", ".o")) for s in B.SOURCES if s != "kv4_attend_kernel.cu"]
     subprocess.run([B._nvcc(), *B.ARCH, "-shared", "-o", lib, obj, *rest, "-lcudart"], check=True, capture_output=True)
-    with_groups = "test_gpu_kv4_shared or test_gpu_kv4_limits or prefix or members or divide or cut or split or nan or allows or requests_and_groups or beside " \
+    with_groups = "test_gpu_kv4_shared or test_gpu_kv4_limits or test_gpu_kv4_lengths or prefix or members or divide or cut or split or nan or allows or requests_and_groups or beside " \
         "or twice or captured or both_caches or rows or parts"
     r = subprocess.run([sys.executable, "-c", CHILD, HERE, lib, with_groups], capture_output=True, text=True, timeout=600, env={**os.environ, "KV4_SHARES": "1"})
     assert r.returncode == 0, r.stdout[-4000:] + r.stderr[-2000:]
