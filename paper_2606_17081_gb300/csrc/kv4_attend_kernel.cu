@@ -131,13 +131,13 @@ constexpr float TILE_128 = 0.45f, TILE_64 = 0.34f;   // of an SM, by cost: of ti
 constexpr float UNIT_8 = 0.122f;                     // of rows' units, of an SM with 8 heads of 128 a chunk: their throughput
 constexpr float UNIT_ALONE = 0.125f, JOB = 6.0f;     // of a worker, by cost, and a job: their latency
 constexpr float TILES_START = 8.0f, ROWS_START = 8.0f;
-__device__ __forceinline__ void split(const Plan& p, Head& h, int64_t items, int longest, bool d128) {
+__device__ __forceinline__ void split(const Plan& p, Head& h, int few_jobs, int64_t items, int longest, bool d128) {   // few_jobs: of warps, with units
   const int n = p.workers[1], teams = p.workers[0] / n;
   int tiles = n;
   h.ctas = n;
   h.whole = 0;
   if (h.total[1] > 0) {
-    const float N = (float)n, jobs = (float)h.jobs[0] * (float)p.chunks;
+    const float N = (float)n, jobs = (float)few_jobs * (float)p.chunks;
     const float x = (d128 ? TILE_128 : TILE_64) * (float)h.total[1];
     const float unit = fmaxf(UNIT_8 * (float)p.chunk * (d128 ? 0.125f : 0.0625f), UNIT_ALONE / (float)teams);
     const float y = unit * ((float)h.total[0] - (float)own_cost(0) * jobs) + JOB / (float)teams * jobs;
@@ -296,11 +296,13 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv4_plan(rs_kv_batch b, Plan p, int
   __shared__ int s_start[PLAN_GROUPS + 1], s_prefix[PLAN_GROUPS];   // of groups: first request; prefix in keys, below 0 where it is not shared
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = b.n_req, G = b.n_groups;
   __shared__ int s_longest;   // tiles of a CTA's job
+  __shared__ int s_empty;     // warps' jobs without units (of members that end inside a prefix)
   __shared__ unsigned long long s_saved;   // by prefixes as jobs of their own
   const bool staged = G <= PLAN_GROUPS;
   if (warp == 0) s_scan[lane] = Sum{};
   if (tid == 0) {
     s_longest = 0;
+    s_empty = 0;
     s_saved = 0;
   }
   __syncthreads();
@@ -429,11 +431,14 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv4_plan(rs_kv_batch b, Plan p, int
     // a request of few jobs is its thread's; a longer one is its warp's
     const bool longer = count > 4;
     int64_t own = 0;
+    int empty = 0;
     if (!longer)
       for (int k = 0; k < count; k++) {
         const Job j = job(k, i, kind, r, key0, alone);
         own += job_cost(kind, j.nt, j.nrows);
+        empty += !kind && j.nt == 0;
       }
+    if (empty) atomicAdd(&s_empty, empty);
     const unsigned many = __ballot_sync(~0u, longer);
     auto others = [&](int src, Lens& o, int& kd, int& k0, int& al) {
       o = Lens{__shfl_sync(~0u, r.q0, src), __shfl_sync(~0u, r.q, src), __shfl_sync(~0u, r.kv, src)};
@@ -514,7 +519,7 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv4_plan(rs_kv_batch b, Plan p, int
       h.total[0] = before.c0 * p.chunks;
       h.total[1] = before.c1 * heads;
     }
-    split(p, h, (int64_t)h.jobs[1] * heads, s_longest, d128);
+    split(p, h, h.jobs[0] - s_empty, (int64_t)h.jobs[1] * heads, s_longest, d128);
     h.q_begin = q_begin;
     h.q_end = q_end;
     h.room = room;

@@ -73,6 +73,15 @@ def test_many_groups(ctx, n):  # noqa: F811
     compare(s, *attend(ctx, s))
 
 
+@pytest.mark.parametrize("inside,behind", [(1000, 1), (300, 20), (40, 0)])
+def test_many_members_inside_the_prefix(ctx, inside, behind):  # noqa: F811
+    """Members that end inside the prefix have no keys of their own; a few stand behind it."""
+    r = random.Random(inside)
+    ctxs = [2048 - r.randint(1, 60) for _ in range(inside)] + [2048 + r.randint(0, 50) for _ in range(behind)]
+    s = Step4(93, [1] * len(ctxs), ctxs, 4, 1, 64, BF, [0, len(ctxs)], [2048])
+    compare(s, *attend(ctx, s))
+
+
 @pytest.mark.parametrize("dim,dtype,prefix,members", [(64, BF, 8192, 44), (64, HF, 96, 40), (128, BF, 128, 6)])
 def test_a_captured_step_of_groups(dim, dtype, prefix, members):
     """Tables with a shared prefix, append and attention captured as one step, replayed on other lengths: members that end
