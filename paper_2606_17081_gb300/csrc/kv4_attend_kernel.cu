@@ -1102,12 +1102,14 @@ __device__ __forceinline__ void join_parts(const KvAttend4Args& a, const Plan& p
 }
 
 // Rows that have parts: of the items that a share's end cuts and, with groups, of the rows
-// that have a prefix job.  Where there are no more than sixteen rows an SM (each may have hundreds of parts), a CTA's 32
-// eights of lanes take every 32nd part of a row.  Else a warp looks for 32 rows where their parts are and joins one
-// after another; neighbouring rows, which have like numbers of parts, are far apart in the grid.  (An eight of lanes a
-// row, neighbours beside each other: 16 us of a step's 44 with 900 rows of up to 40 parts.)  The order in which parts are
-// joined is fixed, so the result does not depend on when they came.  (ONE: all rows of the arrays are so few, and less
-// code has a shorter way to the SM.)
+// that have a prefix job.  Where a CTA has one row at most (each may have hundreds of parts), its 32 eights of lanes take
+// every 32nd part of it.  Else a warp looks for 32 rows where their parts are and joins one after another; neighbouring
+// rows, which have like numbers of parts, are far apart in the grid.  (An eight of lanes a row, neighbours beside each
+// other: 16 us of a step's 44 with 900 rows of up to 40 parts.)  By CTAs and by warps, us a call: one token of 64 heads on 2
+// over 16 160 keys 24 and 60; three rows an SM, 57 tokens of 8 heads on one over 8 000, 32 and 38; four, 76 such, 45 and 44, or
+// over 600, 24 and 22; sixteen, 76 tokens over 600, 38 and 25, a prompt's 304 tokens of 8 heads behind 3 000, 41 and 29.  The
+// order in which parts are joined is fixed, so the result does not depend on when they came.  (ONE: all rows of the
+// arrays are so few, and less code has a shorter way to the SM.)
 // Bound: latency, of reads that depend on one another (head, place, cut, sums, rows): 3 to 6 us.  Three CTAs an SM and four
 // rows on their way (four CTAs: 0 to 2 us more, six to eight: up to 8 us more; eight rows: up to 4 us more).
 template <int D, bool HALF>
@@ -1220,7 +1222,7 @@ __global__ void __launch_bounds__(256, JOINS) k_kv4_join(const __grid_constant__
   behind_stream();
   const int q_end = p.head->room ? p.head->q_end : 0;
   const int64_t from = (int64_t)p.head->q_begin * a.n_heads, rows = (int64_t)q_end * a.n_heads;   // the first, the end
-  if (ONE || rows <= 16 / JOINS * (int64_t)gridDim.x) join_by_cta<D, HALF>(a, p, from, rows, sm);
+  if (ONE || rows - from <= (int64_t)gridDim.x) join_by_cta<D, HALF>(a, p, from, rows, sm);
   else join_by_warp<D, HALF>(a, p, from, rows);
 }
 
@@ -1285,7 +1287,7 @@ cudaError_t run(const KvAttend4Args& a, const Plan& p, int sms, cudaStream_t st)
   e = launch_behind(k, sms, WARPS * 32, RowsLay<D>::SMEM, st, a, p);
   if (e != cudaSuccess) return e;
   const int64_t rows = (int64_t)a.b.n_tokens * a.n_heads;
-  const bool one = rows <= sms * 8ll;
+  const bool one = rows <= (int64_t)sms * JOINS;
   return launch_behind(one ? k_kv4_join<D, HALF, true> : k_kv4_join<D, HALF, false>, (unsigned)(one ? rows : sms * JOINS), 256, 0, st, a, p);
 }
 

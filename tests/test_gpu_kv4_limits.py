@@ -49,3 +49,13 @@ def test_the_largest_scale(ctx, new, ctxs, groups, dtype, unit_power):  # noqa: 
     lse[:, 2:] = far[:, 2:].to(lse)
     s.expected = lambda: (want, far)
     compare(s, out, lse)
+
+
+@pytest.mark.parametrize("rows_an_sm,more", [(1, 0), (2, 0), (3, -1), (3, 0), (3, 1), (4, 0), (16, 0)])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_rows_of_parts_around_where_the_join_changes(ctx, rows_an_sm, more, dim):  # noqa: F811
+    """Up to three rows an SM have a CTA each to join their parts, more of them a warp: a prompt and single tokens, all cut."""
+    heads = 8
+    tokens = rows_an_sm * torch.cuda.get_device_properties(0).multi_processor_count // heads + more
+    s = Step4(83, [tokens - 2, 1, 1], [3000, 9000, 8000], heads, 2, dim, BF)
+    compare(s, *attend(ctx, s))
