@@ -154,16 +154,19 @@ __device__ __forceinline__ void split(const Plan& p, Head& h, int few_jobs, int6
   h.per[1] = share_of(h.total[1], tiles, 1);
 }
 
-// What rows over keys take of an SM, in hundredths of a microsecond or so: of a warp's jobs.
+// What rows over keys cost as a warp's jobs: 8 for a unit of up to 8 rows, by what a unit takes (0.12 us of an SM with heads
+// of 128, 0.06 with 64).
 __device__ __forceinline__ int64_t few_take(int64_t rows, int keys) {
   const int64_t full = rows / FEW, rest = rows - full * FEW;
   return units_of(0, keys) * (full * 13 + (rest > 8 ? 13 : rest > 0 ? 8 : 0)) + 8 * (full + 1);
 }
 
 // Whether sharing prefixes is worth another job's way through memory for each row, as it saves `saved` (of few_take) a kv
-// head: from 7 us of all SMs on.  (Work less, and a call with and without, us: 8 requests of 4 rows on 1 024 keys 0.6,
-// 19.8 and 16.6; 98 of 5 on 1 040, one kv head, 1.4, 35.8 and 26.7; 4 of 4 on 16 384 5.1, 30.6 and 27.1; 2 of 4 on 65 536
-// 8.6, 34.7 and 42.1; 40 of 4 on 2 048 9.4, 39.7 and 42.6.)
+// head: from 7 hundred an SM on.  The limit is of work by these costs, not of a time: with heads of 128 it is some 10 us, with 64
+// 5 to 6, as starts and joins are quicker there too.  Hundreds saved an SM, and us a call with and without, for heads of 128 and
+// of 64: 8 requests of 4 rows on 1 024 keys 0.6: 18.6 and 16.5; 15.4 and 14.4.  98 of 5 on 1 040, one kv head, 1.5: 30.3 and 22.5; 26.3 and
+// 19.4.  40 of 4 on 1 024 4.7: 29.9 and 29.5; 26.0 and 24.0.  4 of 4 on 16 384 5.1: 30.5 and 27.5; 19.9 and 21.2.  64 of 8 on 1 024 7.1: 35.3 and
+// 41.7; 30.9 and 31.6.  2 of 4 on 65 536 8.6: 34.9 and 41.8; 23.0 and 27.3.  40 of 4 on 2 048 9.6: 31.3 and 36.2; 26.3 and 28.2.
 #ifndef KV4_WORTH   // (a test builds with 0: every prefix is shared that costs less so)
 #define KV4_WORTH 700
 #endif
@@ -312,7 +315,7 @@ __global__ void __launch_bounds__(NT_PLAN) k_kv4_plan(rs_kv_batch b, Plan p, int
   auto lens = [&](int i) { return lens_of(b, i); };
   auto kind_of = [&](int64_t rows) { return rows > p.few_max ? 1 : 0; };
   auto prefix_of = [&](int g) { return min(max(b.prefix_len[g], 0) & ~15, max_keys & ~15); };
-  // what rows over keys take of an SM, in hundredths of a microsecond or so
+  // what rows over keys cost, in the units of few_take
   auto takes = [&](int64_t rows, int keys) -> int64_t {
     if (rows > p.few_max) {
       const int64_t full = rows / MANY, rest = rows - full * MANY;
