@@ -439,7 +439,7 @@ rs_status poa_estimate_noalloc(const rs_config* cfg, const rs_records* records, 
  * them (kv_attend).  The paper assumes a serving engine here and gives no
  * kernels; layouts and rules below are this library's.
  *
- * Of the context these calls use the stream, and kv_attend a workspace and a flag;
+ * Of the context these calls use the stream, and the attentions a workspace and a flag;
  * W, the cache sizes and the instances of route_init play no part in them.
  *
  * A step: n_req requests, request i with q_len[i] >= 0 new tokens after
@@ -449,9 +449,12 @@ rs_status poa_estimate_noalloc(const rs_config* cfg, const rs_records* records, 
  * fixed size).  Token t of request i stands at position kv_len[i] - q_len[i]
  * + t.  All calls are asynchronous on the context stream, read lengths and
  * tables on the device only, and neither read nor write outside the arrays
- * described here, whatever the lengths and tables hold.  The workspace of
- * kv_attend (some 20 to 40 MB, and with groups 2 n_tokens n_heads (4 head_dim +
- * 8) bytes more) grows at a call larger than those before it (cudaMalloc), so a
+ * described here, whatever the lengths and tables hold.  The attentions share a
+ * workspace: for kv_attend some 20 to 40 MB, and with groups 2 n_tokens n_heads
+ * (4 head_dim + 8) bytes more; for kv_attend4 with heads of 128 some 41 MB, 82 MB
+ * where n_tokens times n_heads / n_kv_heads is above 32 (with heads of 64 half of
+ * it), 4 n_tokens n_heads bytes, and with groups 2 n_tokens n_heads (4 head_dim + 18)
+ * more.  It grows at a call larger than those before it (cudaMalloc), so a
  * stream capture follows one such call outside it (else RS_ERR_STATE, without
  * a launch); what a capture holds stays until route_destroy, and is shared:
  * replays and calls of one context must not overlap on the GPU. */
@@ -588,7 +591,7 @@ typedef struct {
 /* As kv_append, K and V in dtype (RS_BF16 or RS_FP16), into a cache in 4 bits.  Of a group's
  * 16 values x: u = x / unit, scale = min(max |u| / 6, 448) rounded to nearest (ties to even),
  * code = u / scale rounded to nearest (ties to the even code), at most 6; a scale of 0 has
- * codes 0.  Infinities end as +-2688 units; a group with a NaN gets a NaN scale.  Rows with a
+ * codes of +-0.  Infinities end as +-2688 units; a group with a NaN gets a NaN scale.  Rows with a
  * slot outside the cache are skipped.  The slots of a call should differ (kv_tables' do): rows
  * with one slot leave that token's values unspecified. */
 rs_status kv_append4(rs_ctx* ctx, const rs_kv_cache4* cache, int32_t dtype, const void* k_dev,
@@ -604,8 +607,8 @@ rs_status kv_read4(rs_ctx* ctx, const rs_kv_cache4* cache, const int64_t* slots_
 
 /* kv_attend over a cache in 4 bits: the same formulas, batches, groups, masks, empty rows and
  * refusals, q and out in dtype.  K and V enter the products as they are held; scores, softmax
- * statistics and sums are in 32 bits, the weights p_j are rounded once to 11 significant bits for
- * the product with V (weights below 2^-27 of their row's largest may lose more, or all), and out
+ * statistics and sums are in 32 bits; for the product with V a weight p_j keeps 11 significant bits
+ * down to 2^-17 of its row's largest, and below that is off by up to 2^-28 of the largest; out is rounded
  * once at the end.  A q in bf16 enters as it is, except elements below 2^-30 of their row's largest,
  * which are rounded to 2^-38 of that.  Any scale that is finite and > 0 will do; where scores are past
  * 2^127 in size, lse is unspecified. */

@@ -1417,12 +1417,12 @@ rs_status kv_append(rs_ctx* ctx, const rs_kv_cache* cache, const void* k_dev, co
   return RS_OK;
 }
 
-// Whether a kv_attend that has ended gave up; each is reported once.
+// Whether an attention that has ended gave up; each is reported once.
 static rs_status kv_gave_up(rs_ctx* ctx) {
   volatile int32_t* const err = ctx->kv_err;
   if (!err || !*err) return RS_OK;
   *err = 0;
-  return fail(ctx, RS_ERR_TIMEOUT, "an earlier kv_attend gave up waiting for its own copies or products");
+  return fail(ctx, RS_ERR_TIMEOUT, "an earlier kv_attend or kv_attend4 gave up waiting for its own copies or products");
 }
 
 rs_status kv_status(rs_ctx* ctx) {
