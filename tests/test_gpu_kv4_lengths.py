@@ -1,7 +1,7 @@
 """kv_attend4 on starts and lengths that do not fit together, in steps of every size (bounds: kv4_reference.compare)."""
 import pytest
 
-from kv4_reference import Step4, compare
+from kv4_reference import Step4, compare, empty_cache
 from paper_2606_17081_gb300 import routesim as rs
 
 pytestmark = pytest.mark.gpu
@@ -71,3 +71,14 @@ def test_lengths_that_do_not_fit_together_stay_inside_the_arrays(ctx, new, ctxs,
         again, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
         rs.kv_attend4(ctx.h, cache, batch, q, s.scale, again, lse)
     compare(s, again, lse)
+
+
+@pytest.mark.parametrize("rows", [1, 5, 40, 700])
+def test_no_request_in_steps_of_every_size(ctx, rows):  # noqa: F811
+    cache = empty_cache(rs, 4, 2, 64)
+    z = torch.zeros(0, dtype=torch.int32, device="cuda")
+    b = rs.KVBatch(z.reshape(0, 3), torch.zeros(1, dtype=torch.int32, device="cuda"), z, rows)
+    q = torch.ones(rows, 16, 64, dtype=BF, device="cuda")
+    out, lse = torch.ones_like(q), torch.ones(rows, 16, device="cuda")
+    rs.kv_attend4(ctx.h, cache, b, q, 1.0, out, lse)
+    assert (out == 0).all() and (lse == -float("inf")).all()
