@@ -577,8 +577,9 @@ struct RowsLay {
 // HBM takes for the codes.)
 // Bound: HBM with up to 8 rows: 128 contexts of 2 048 to 24 576, 8 kv heads of 128, 1.33 GB in 231 us, 5.76 TB/s; a page
 // takes an SM 119 clocks, 101 at the copy rate, and 292 instructions (73 clocks of issue), of which the conversions,
-// 64, and the scales' products, 64, go through pipes of half rate.  With 16 rows mma.sync (1 024 multiply-adds a clock
-// and SM, an eighth of tcgen05's) and registers bound it: 370 us.
+// 64, and the scales' products, 64, go through pipes of half rate.  With 9 to 16 rows the same contexts take 370 us, 191
+// clocks a page: a page at a time, a stage less, q from shared memory, and at 128 registers 72 bytes of spills; mma.sync
+// (1 024 multiply-adds a clock and SM) is a third of it.
 // Measured and not kept: a page at a time (247 against 237 us a call); this function out of line (259 us).
 template <int D, bool HALF, int N>
 __device__ __forceinline__ void rows_segment(const KvAttend4Args& a, const Plan& p, const Job& job, int head, int t0, int t1, int worker,

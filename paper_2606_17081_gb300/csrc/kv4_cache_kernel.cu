@@ -86,9 +86,9 @@ __device__ __forceinline__ void load16(const uint16_t* src, uint32_t* u) {
 
 // 2^team_log threads have a row: each UNR groups of 16 elements of K and of V at a time, whose
 // loads are on their way together.  (Head sizes are powers of two: a group's head is a shift.)
-// Bound: HBM, 2 bytes an element read and 9/16 written; a thread's address arithmetic is half of its
-// instructions.  16 001 rows of 8 heads of 128 (66 MB in, 18 out): 17.5 us, 4.8 TB/s; appended and read back
-// 26.8 us, against 41 us where every group of K or V had a thread and a row's address of its own.
+// Bound: the loads' latency and the instructions, of which a thread's address arithmetic is half; 2 bytes an element are
+// read and 9/16 written, and DRAM is busy half of the time (most of what is written stays in L2).  16 001 rows of 8 heads of
+// 128 (66 MB in, 18 out): 17.5 us, 4.8 TB/s, where the copy rate would take 12.5; appended and read back 26.8 us, against 41 us where every group of K or V had a thread and a row's address of its own.
 template <int D, bool HALF, bool WIDE, int UNR>
 __global__ void __launch_bounds__(256) k_kv_append4(rs_kv_cache4 c, const uint16_t* k, const uint16_t* v, int64_t ts, int64_t hs,
                                                     int n_tokens, const int64_t* slots, int team_log, float inv_k, float inv_v) {
@@ -158,7 +158,8 @@ __device__ __forceinline__ void values8(uint32_t w, uint32_t s, float unit, uint
 
 // 2^team_log threads have a row: each UNR pieces of eight elements of K and of V at a time,
 // whose loads are on their way together.
-// Bound: HBM, 9/16 byte an element read and 2 written.  60 000 rows of 8 heads of 64 (35 MB in, 123 out): 27.5 us,
+// Bound: the instructions (two conversions, a product and a rounding a pair) and the scales' partial sectors beside 9/16 byte
+// an element read and 2 written; DRAM is busy 42% of the time, as half of what is written stays in L2.  60 000 rows of 8 heads of 64 (35 MB in, 123 out): 27.5 us,
 // 5.75 TB/s (UNR 1: 30.0 us, 4: 32.1 us; a piece a thread with an address of its own: 51 us).
 template <int D, bool HALF, bool WIDE, int UNR>
 __global__ void __launch_bounds__(256) k_kv_read4(rs_kv_cache4 c, uint16_t* k, uint16_t* v, int64_t ts, int64_t hs, int n_tokens,
